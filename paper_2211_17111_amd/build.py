@@ -22,8 +22,8 @@ LIB_PATH = os.path.join(PKG, LIB_NAME)
 
 ARCH = "gfx950"
 SOURCES = ["prepare.hip", "prepare_plan.hip", "schedule_local.hip", "forward.hip", "forward_strips.hip", "forward_dense.hip", "backward.hip", "softmax.hip",
-           "geometry.hip",
-           "api.cpp"]
+           "geometry.hip", "rows_sort.hip", "rows_route.hip", "rows_move.hip", "rows_embed.hip",
+           "api.cpp", "rows_api.cpp"]
 # measurement probe for bench.py, built into a library of its own
 PROBE_SOURCE = "stream_probe.hip"
 PROBE_LIB = os.path.join(PKG, "libbevpool_probe.so")
@@ -135,7 +135,7 @@ def build_sanitized(verbose: bool = False) -> str:
     ABI tests' argument-validation paths (no GPU needed).  Rebuilt only when
     a source or header is newer than it."""
     os.makedirs(SAN_DIR, exist_ok=True)
-    inputs = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(INCLUDE, "bevpool.h")]
+    inputs = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(INCLUDE, f) for f in os.listdir(INCLUDE)]
     if os.path.exists(SAN_LIB) and os.path.getmtime(SAN_LIB) >= max(map(os.path.getmtime, inputs)):
         return SAN_LIB
     cc = hipcc()

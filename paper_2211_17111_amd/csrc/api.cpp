@@ -12,6 +12,7 @@
 
 #include "bevpool.h"
 #include "internal.h"
+#include "status.h"
 
 namespace bevpool {
 
@@ -27,16 +28,9 @@ Dims dims_of(const bevpool_shape& s) {
   return d;
 }
 
-}  // namespace bevpool
-
 namespace {
-
 thread_local std::string g_last_error;
-
-constexpr int64_t kIndexLimit = int64_t(1) << 31;
-constexpr int64_t kMaxC = 1024;
-
-int fail(int status, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+}
 
 int fail(int status, const char* fmt, ...) {
   char buf[512];
@@ -52,6 +46,24 @@ int ok() {
   g_last_error.clear();
   return BEVPOOL_OK;
 }
+
+int from_hip(hipError_t e, const char* what) {
+  if (e == hipSuccess) return ok();
+  return fail(BEVPOOL_ELAUNCH, "%s: %s (%s)", what, hipGetErrorName(e), hipGetErrorString(e));
+}
+
+const char* last_error() { return g_last_error.c_str(); }
+
+}  // namespace bevpool
+
+namespace {
+
+using bevpool::fail;
+using bevpool::from_hip;
+using bevpool::ok;
+
+constexpr int64_t kIndexLimit = int64_t(1) << 31;
+constexpr int64_t kMaxC = 1024;
 
 int check_shape(const bevpool_shape* s, bevpool::Dims* out) {
   if (s == nullptr) return fail(BEVPOOL_EINVAL, "shape is NULL");
@@ -80,16 +92,6 @@ int check_dtypes(int in_dtype, int out_dtype) {
   if (in_dtype == BEVPOOL_F32 && out_dtype == BEVPOOL_F16)
     return fail(BEVPOOL_EDTYPE, "float32 inputs with a float16 output are not supported");
   return BEVPOOL_OK;
-}
-
-#define REQUIRE_PTR(p)                                          \
-  do {                                                          \
-    if ((p) == nullptr) return fail(BEVPOOL_EINVAL, #p " is NULL"); \
-  } while (0)
-
-int from_hip(hipError_t e, const char* what) {
-  if (e == hipSuccess) return ok();
-  return fail(BEVPOOL_ELAUNCH, "%s: %s (%s)", what, hipGetErrorName(e), hipGetErrorString(e));
 }
 
 int check_counts(const bevpool::Dims& d, int32_t n_valid, int32_t n_intervals) {
@@ -148,7 +150,7 @@ const char* bevpool_strerror(int status) {
   }
 }
 
-const char* bevpool_last_error(void) { return g_last_error.c_str(); }
+const char* bevpool_last_error(void) { return bevpool::last_error(); }
 
 int bevpool_prepare_workspace_size(const bevpool_shape* shape, size_t* bytes) {
   bevpool::Dims d;

@@ -1,0 +1,499 @@
+"""Row operators of libbevpool.so (include/bevpool_rows.h): router, dispatch
+and combine of expert layers, embedding lookup, and the stable key sort they
+share.
+
+They are the moves of the pooling path for keys that are expert ids or row
+ids: ``sort_keys`` orders slots by key as ``prepare`` orders frustum points by
+cell, and rows are read through that order and summed without atomics.  Keys
+outside their range (padding, a token past an expert's capacity) are dropped:
+they sort last, their rows are zero and carry no gradient.
+
+``*_forward`` and ``*_backward`` allocate their outputs and launch the kernels;
+``route``, ``dispatch``, ``combine`` and ``embed`` are their differentiable
+forms.  A layer of experts reads
+
+    weights, ids = route(logits, k)
+    rows, plan = dispatch(x, ids, n_experts)      # rows of expert e:
+    y = experts(rows, plan.offsets)               #   offsets[e] .. offsets[e+1]
+    out = combine(y, weights, plan)
+
+Matrices may have any distance between their rows (a slice of a wider matrix,
+one row expanded); elements of a row are neighbours.  Everything runs on the
+tensors' device and its current stream, or on ``stream``, which the inputs then
+have to be ready on.  No call synchronises or reads back.
+"""
+
+from __future__ import annotations
+
+import ctypes
+from dataclasses import dataclass
+
+import torch
+from torch.autograd.function import once_differentiable
+
+from . import bevpool as _bp
+
+BEVPOOL_BF16 = 2
+BEVPOOL_KEY_I32, BEVPOOL_KEY_I64 = 0, 1
+
+_DTYPE_CODE = {torch.float32: _bp.BEVPOOL_F32, torch.float16: _bp.BEVPOOL_F16, torch.bfloat16: BEVPOOL_BF16}
+_KEY_CODE = {torch.int32: BEVPOOL_KEY_I32, torch.int64: BEVPOOL_KEY_I64}
+
+_vp, _i32, _i64, _int, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_int, ctypes.c_size_t
+_ARGTYPES = {
+    "bevpool_sort_keys_workspace_size": [_i64, _i64, ctypes.POINTER(_sz)],
+    "bevpool_sort_keys": [_i64, _i64, _int, _vp, _vp, _vp, _vp, _vp, _sz, _vp],
+    "bevpool_route_forward": [_i64, _i32, _i32, _int, _vp, _i64, _int, _vp, _vp, _vp],
+    "bevpool_route_backward": [_i64, _i32, _i32, _int, _vp, _vp, _i64, _vp, _vp, _int, _vp, _vp],
+    "bevpool_dispatch_forward": [_i64, _i32, _i64, _i64, _int, _vp, _i64, _int, _vp, _vp, _vp, _vp, _vp, _vp, _sz,
+                                 _vp],
+    "bevpool_dispatch_rows": [_i64, _i32, _i64, _int, _vp, _i64, _vp, _vp, _vp, _vp],
+    "bevpool_dispatch_backward": [_i64, _i32, _i64, _int, _vp, _i64, _vp, _vp, _vp, _vp],
+    "bevpool_combine_forward": [_i64, _i32, _i64, _int, _int, _int, _vp, _i64, _vp, _vp, _vp, _vp, _vp],
+    "bevpool_combine_backward": [_i64, _i32, _i64, _int, _int, _int, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp,
+                                 _vp],
+    "bevpool_embed_forward": [_i64, _i64, _i64, _int, _int, _vp, _i64, _int, _vp, ctypes.c_float, _vp, _vp],
+    "bevpool_embed_backward_workspace_size": [_i64, _i64, _i64, ctypes.POINTER(_sz)],
+    "bevpool_embed_backward": [_i64, _i64, _i64, _int, _int, _vp, _i64, _int, _vp, ctypes.c_float, _vp, _vp, _sz,
+                               _vp],
+}
+
+_lib = None
+
+
+def load_library() -> ctypes.CDLL:
+    """libbevpool.so with the row operators' signatures (raises if it has not been built)."""
+    global _lib
+    if _lib is None:
+        lib = _bp.load_library()
+        for name, argtypes in _ARGTYPES.items():
+            f = getattr(lib, name)
+            f.restype, f.argtypes = _int, argtypes
+        _lib = lib
+    return _lib
+
+
+def _call(name: str, *args) -> None:
+    lib = _lib or load_library()
+    status = getattr(lib, name)(*args)
+    if status != 0:
+        _bp._check(lib, status, name)
+
+
+def _size(name: str, *args) -> int:
+    n = _sz(0)
+    _call(name, *args, ctypes.byref(n))
+    return n.value
+
+
+# ----------------------------------------------------------------- arguments
+
+def _device(t, name: str) -> torch.device:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA (HIP) tensor")
+    return t.device
+
+
+def _matrix(t, name: str, dev: torch.device, dtype=None, shape=None) -> int:
+    """Checks a matrix whose rows are runs of neighbouring elements; the
+    distance between its rows."""
+    if not isinstance(t, torch.Tensor) or t.device != dev:
+        raise ValueError(f"{name} must be a tensor on {dev}")
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != shape):
+        raise ValueError(f"{name} must be {shape or 'a matrix'}, got {tuple(t.shape)}")
+    if t.dtype not in _DTYPE_CODE or (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{name} must be {dtype or 'float32, float16 or bfloat16'}, got {t.dtype}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: the elements of a row must be neighbours (stride {t.stride(1)})")
+    return t.stride(0)
+
+
+def _dense(t, name: str, dev: torch.device, dtypes, shape=None) -> None:
+    if not isinstance(t, torch.Tensor) or t.device != dev:
+        raise ValueError(f"{name} must be a tensor on {dev}")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} must be one of {[str(d) for d in dtypes]}, got {t.dtype}")
+    if shape is not None and tuple(t.shape) != shape:
+        raise ValueError(f"{name} must be {shape}, got {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _elsewhere(dev: torch.device, stream, *inputs):
+    """A context in which dev and `stream` are current, or None where they
+    already are: allocations and launches then belong to that stream."""
+    if stream is None:
+        return None if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream), device=dev)
+    if stream.device != dev:
+        raise ValueError(f"the stream is on {stream.device}, the tensors on {dev}")
+    for t in inputs:  # (their memory must outlive the work on that stream)
+        if isinstance(t, torch.Tensor) and t.is_cuda:
+            t.record_stream(stream)
+    return torch.cuda.stream(stream)
+
+
+@dataclass
+class KeyOrder:
+    """Stable order of n slots by key: ``order[q]`` the slot at place q,
+    ``position[s]`` the place of slot s, ``offsets[v]`` the first place of key
+    v, ``offsets[n_keys]`` the number of kept slots (dropped ones lie behind)."""
+    order: torch.Tensor
+    position: torch.Tensor
+    offsets: torch.Tensor
+    n_keys: int
+
+    def _check(self, dev: torch.device, n: int) -> int:
+        """Address of the number of kept slots."""
+        _dense(self.position, "position", dev, (torch.int32,))
+        _dense(self.offsets, "offsets", dev, (torch.int32,))
+        if self.position.numel() != n or self.offsets.numel() != self.n_keys + 1:
+            raise ValueError(f"the order has {self.position.numel()} slots and {self.offsets.numel()} offsets; "
+                             f"{n} slots and {self.n_keys + 1} offsets are needed")
+        return self.offsets.data_ptr() + 4 * self.n_keys
+
+
+def _key_order(n: int, n_keys: int, dev: torch.device):
+    i32 = dict(dtype=torch.int32, device=dev)
+    plan = KeyOrder(torch.empty(n, **i32), torch.empty(n, **i32), torch.empty(n_keys + 1, **i32), n_keys)
+    nbytes = _size("bevpool_sort_keys_workspace_size", n, n_keys)
+    return plan, torch.empty(nbytes, dtype=torch.uint8, device=dev), nbytes
+
+
+# --------------------------------------------------------------- key sorting
+
+def sort_keys(keys: torch.Tensor, n_keys: int, stream=None) -> KeyOrder:
+    """Stable order of integer keys (any shape, int32 or int64) in [0, n_keys);
+    keys outside are dropped."""
+    dev = _device(keys, "keys")
+    _dense(keys, "keys", dev, _KEY_CODE)
+    ctx = _elsewhere(dev, stream, keys)
+    if ctx is not None:
+        with ctx:
+            return sort_keys(keys, n_keys)
+    n = keys.numel()
+    plan, ws, nbytes = _key_order(n, n_keys, dev)
+    _call("bevpool_sort_keys", n, n_keys, _KEY_CODE[keys.dtype], keys.data_ptr(), plan.order.data_ptr(),
+          plan.position.data_ptr(), plan.offsets.data_ptr(), ws.data_ptr(), nbytes, _bp._stream(None))
+    return plan
+
+
+# -------------------------------------------------------------------- router
+
+def route_forward(logits: torch.Tensor, k: int, renormalise: bool = True, stream=None):
+    """(weights, ids) of the k largest logits (T, E) of every row: ids (T, k)
+    int32 by descending logit, equal logits by index, -1 where fewer than k are
+    above -inf; weights (T, k) float32, their softmax over the chosen
+    (renormalise) or over all experts."""
+    dev = _device(logits, "logits")
+    stride = _matrix(logits, "logits", dev)
+    ctx = _elsewhere(dev, stream, logits)
+    if ctx is not None:
+        with ctx:
+            return route_forward(logits, k, renormalise)
+    T, E = logits.shape
+    weights = torch.empty((T, k), dtype=torch.float32, device=dev)
+    ids = torch.empty((T, k), dtype=torch.int32, device=dev)
+    _call("bevpool_route_forward", T, E, k, _DTYPE_CODE[logits.dtype], logits.data_ptr(), stride, int(renormalise),
+          weights.data_ptr(), ids.data_ptr(), _bp._stream(None))
+    return weights, ids
+
+
+def route_backward(grad_weights: torch.Tensor, logits: torch.Tensor, weights: torch.Tensor, ids: torch.Tensor,
+                   renormalise: bool = True, stream=None) -> torch.Tensor:
+    """Gradient (T, E) of the logits, in their type."""
+    dev = _device(logits, "logits")
+    stride = _matrix(logits, "logits", dev)
+    T, E = logits.shape
+    k = ids.shape[-1]
+    _dense(grad_weights, "grad_weights", dev, (torch.float32,), (T, k))
+    _dense(weights, "weights", dev, (torch.float32,), (T, k))
+    _dense(ids, "ids", dev, (torch.int32,), (T, k))
+    ctx = _elsewhere(dev, stream, grad_weights, logits, weights, ids)
+    if ctx is not None:
+        with ctx:
+            return route_backward(grad_weights, logits, weights, ids, renormalise)
+    grad = torch.empty((T, E), dtype=logits.dtype, device=dev)
+    _call("bevpool_route_backward", T, E, k, _DTYPE_CODE[logits.dtype], grad_weights.data_ptr(), logits.data_ptr(),
+          stride, weights.data_ptr(), ids.data_ptr(), int(renormalise), grad.data_ptr(), _bp._stream(None))
+    return grad
+
+
+# ------------------------------------------------------- dispatch and combine
+
+def dispatch_forward(x: torch.Tensor, ids, n_experts: int | None = None, stream=None):
+    """(rows, plan): the rows of x (T, C) in the order of their experts, one for
+    every slot of ids (T, k), and that order.  Rows of dropped slots lie behind
+    the kept ones and are zero.  ``ids`` may also be the KeyOrder of an earlier
+    call with T rows."""
+    dev = _device(x, "x")
+    stride = _matrix(x, "x", dev)
+    T, C = x.shape
+    if isinstance(ids, KeyOrder):
+        plan = ids
+        n = plan.position.numel()
+        k = n // T if T else 1
+        kept = plan._check(dev, T * k)
+    else:
+        _dense(ids, "ids", dev, _KEY_CODE)
+        if ids.dim() != 2 or ids.shape[0] != T:
+            raise ValueError(f"ids must be ({T}, k), got {tuple(ids.shape)}")
+        if n_experts is None:
+            raise ValueError("n_experts is needed with ids")
+        plan = None
+        k, n = ids.shape[1], ids.numel()
+    ctx = _elsewhere(dev, stream, x, *((ids,) if plan is None else (plan.position, plan.offsets)))
+    if ctx is not None:
+        with ctx:
+            return dispatch_forward(x, ids, n_experts)
+    out = torch.empty((n, C), dtype=x.dtype, device=dev)
+    if plan is not None:
+        _call("bevpool_dispatch_rows", T, k, C, _DTYPE_CODE[x.dtype], x.data_ptr(), stride, plan.position.data_ptr(),
+              kept, out.data_ptr(), _bp._stream(None))
+        return out, plan
+    plan, ws, nbytes = _key_order(n, n_experts, dev)
+    _call("bevpool_dispatch_forward", T, k, C, n_experts, _DTYPE_CODE[x.dtype], x.data_ptr(), stride,
+          _KEY_CODE[ids.dtype], ids.data_ptr(), plan.order.data_ptr(), plan.position.data_ptr(),
+          plan.offsets.data_ptr(), out.data_ptr(), ws.data_ptr(), nbytes, _bp._stream(None))
+    return out, plan
+
+
+def _tokens(rows: torch.Tensor, k: int) -> int:
+    if k < 1 or rows.shape[0] % k:
+        raise ValueError(f"{rows.shape[0]} rows are not a multiple of k = {k}")
+    return rows.shape[0] // k
+
+
+def dispatch_backward(grad_rows: torch.Tensor, plan: KeyOrder, k: int, stream=None) -> torch.Tensor:
+    """Gradient (T, C) of x from that of the dispatched rows (T k, C)."""
+    dev = _device(grad_rows, "grad_rows")
+    stride = _matrix(grad_rows, "grad_rows", dev)
+    T = _tokens(grad_rows, k)
+    kept = plan._check(dev, T * k)
+    ctx = _elsewhere(dev, stream, grad_rows, plan.position, plan.offsets)
+    if ctx is not None:
+        with ctx:
+            return dispatch_backward(grad_rows, plan, k)
+    C = grad_rows.shape[1]
+    grad = torch.empty((T, C), dtype=grad_rows.dtype, device=dev)
+    _call("bevpool_dispatch_backward", T, k, C, _DTYPE_CODE[grad_rows.dtype], grad_rows.data_ptr(), stride,
+          plan.position.data_ptr(), kept, grad.data_ptr(), _bp._stream(None))
+    return grad
+
+
+def combine_forward(rows: torch.Tensor, weights: torch.Tensor, plan: KeyOrder, out_dtype=None,
+                    stream=None) -> torch.Tensor:
+    """(T, C): the sum of every token's kept rows, out of rows (T k, C) in the
+    order of their experts, times its weights (T, k; float32 or rows' type).
+    out_dtype: rows' type (default) or float32."""
+    dev = _device(rows, "rows")
+    stride = _matrix(rows, "rows", dev)
+    _dense(weights, "weights", dev, (torch.float32, rows.dtype))
+    n, C = rows.shape
+    if weights.dim() != 2 or weights.numel() != n:
+        raise ValueError(f"weights must be (T, k) for {n} rows, got {tuple(weights.shape)}")
+    T, k = weights.shape
+    kept = plan._check(dev, n)
+    odt = out_dtype or rows.dtype
+    if odt not in (rows.dtype, torch.float32):
+        raise ValueError(f"out_dtype must be {rows.dtype} or float32, got {odt}")
+    ctx = _elsewhere(dev, stream, rows, weights, plan.position, plan.offsets)
+    if ctx is not None:
+        with ctx:
+            return combine_forward(rows, weights, plan, out_dtype)
+    out = torch.empty((T, C), dtype=odt, device=dev)
+    _call("bevpool_combine_forward", T, k, C, _DTYPE_CODE[rows.dtype], _DTYPE_CODE[odt], _DTYPE_CODE[weights.dtype],
+          rows.data_ptr(), stride, weights.data_ptr(), plan.position.data_ptr(), kept, out.data_ptr(),
+          _bp._stream(None))
+    return out
+
+
+def combine_backward(grad_out: torch.Tensor, rows: torch.Tensor, weights: torch.Tensor, plan: KeyOrder,
+                     need_rows: bool = True, need_weights: bool = True, stream=None):
+    """(grad_rows, grad_weights) of combine_forward, in the types of rows and
+    weights; None for one that is not needed."""
+    dev = _device(rows, "rows")
+    stride = _matrix(rows, "rows", dev)
+    _dense(weights, "weights", dev, (torch.float32, rows.dtype))
+    n, C = rows.shape
+    if weights.dim() != 2 or weights.numel() != n:
+        raise ValueError(f"weights must be (T, k) for {n} rows, got {tuple(weights.shape)}")
+    T, k = weights.shape
+    grad_stride = _matrix(grad_out, "grad_out", dev, shape=(T, C))
+    if grad_out.dtype not in (rows.dtype, torch.float32):
+        raise ValueError(f"grad_out must be {rows.dtype} or float32, got {grad_out.dtype}")
+    kept = plan._check(dev, n)
+    ctx = _elsewhere(dev, stream, grad_out, rows, weights, plan.position, plan.offsets)
+    if ctx is not None:
+        with ctx:
+            return combine_backward(grad_out, rows, weights, plan, need_rows, need_weights)
+    grad_rows = torch.empty((n, C), dtype=rows.dtype, device=dev) if need_rows else None
+    grad_weights = torch.empty((T, k), dtype=weights.dtype, device=dev) if need_weights else None
+    _call("bevpool_combine_backward", T, k, C, _DTYPE_CODE[rows.dtype], _DTYPE_CODE[grad_out.dtype],
+          _DTYPE_CODE[weights.dtype], grad_out.data_ptr(), grad_stride, rows.data_ptr(), stride, weights.data_ptr(),
+          plan.position.data_ptr(), kept, grad_rows.data_ptr() if need_rows else None,
+          grad_weights.data_ptr() if need_weights else None, _bp._stream(None))
+    return grad_rows, grad_weights
+
+
+# ----------------------------------------------------------------- embedding
+
+def embed_forward(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, out_dtype=None,
+                  stream=None) -> torch.Tensor:
+    """scale * table[ids] of shape ids.shape + (C,); zeros for ids outside the
+    table.  out_dtype: the table's type (default) or float32."""
+    dev = _device(table, "table")
+    stride = _matrix(table, "table", dev)
+    _dense(ids, "ids", dev, _KEY_CODE)
+    odt = out_dtype or table.dtype
+    if odt not in (table.dtype, torch.float32):
+        raise ValueError(f"out_dtype must be {table.dtype} or float32, got {odt}")
+    ctx = _elsewhere(dev, stream, table, ids)
+    if ctx is not None:
+        with ctx:
+            return embed_forward(table, ids, scale, out_dtype)
+    V, C = table.shape
+    out = torch.empty(ids.shape + (C,), dtype=odt, device=dev)
+    _call("bevpool_embed_forward", ids.numel(), V, C, _DTYPE_CODE[table.dtype], _DTYPE_CODE[odt], table.data_ptr(),
+          stride, _KEY_CODE[ids.dtype], ids.data_ptr(), scale, out.data_ptr(), _bp._stream(None))
+    return out
+
+
+def embed_backward(grad_out: torch.Tensor, ids: torch.Tensor, table_rows: int, scale: float = 1.0, grad_dtype=None,
+                   stream=None) -> torch.Tensor:
+    """Gradient (table_rows, C) of the table, zeros in rows that no id names.
+    grad_dtype: grad_out's type (default), float32, or any type when grad_out
+    is float32."""
+    dev = _device(ids, "ids")
+    _dense(ids, "ids", dev, _KEY_CODE)
+    if not isinstance(grad_out, torch.Tensor) or grad_out.dim() < 1 or grad_out.shape[:-1] != ids.shape:
+        raise ValueError(f"grad_out must be {tuple(ids.shape)} + (C,)")
+    if grad_out.dim() != 2:
+        if not grad_out.is_contiguous():
+            raise ValueError("grad_out must be contiguous or a matrix")
+        grad_out = grad_out.view(ids.numel(), grad_out.shape[-1])
+    stride = _matrix(grad_out, "grad_out", dev)
+    gdt = grad_dtype or grad_out.dtype
+    if gdt not in _DTYPE_CODE or (gdt != grad_out.dtype and torch.float32 not in (gdt, grad_out.dtype)):
+        raise ValueError(f"grad_dtype {gdt} does not go with a grad_out of {grad_out.dtype}")
+    ctx = _elsewhere(dev, stream, grad_out, ids)
+    if ctx is not None:
+        with ctx:
+            return embed_backward(grad_out.view(ids.shape + grad_out.shape[-1:]) if ids.dim() != 1 else grad_out, ids,
+                                  table_rows, scale, grad_dtype)
+    n, C = grad_out.shape
+    grad = torch.empty((table_rows, C), dtype=gdt, device=dev)
+    nbytes = _size("bevpool_embed_backward_workspace_size", n, table_rows, C)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    _call("bevpool_embed_backward", n, table_rows, C, _DTYPE_CODE[grad_out.dtype], _DTYPE_CODE[gdt],
+          grad_out.data_ptr(), stride, _KEY_CODE[ids.dtype], ids.data_ptr(), scale, grad.data_ptr(), ws.data_ptr(),
+          nbytes, _bp._stream(None))
+    return grad
+
+
+# ------------------------------------------------------- differentiable forms
+
+class RouteFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, k, renormalise):
+        weights, ids = route_forward(logits, k, renormalise)
+        ctx.renormalise = renormalise
+        ctx.save_for_backward(logits, weights, ids)
+        ctx.mark_non_differentiable(ids)
+        ctx.set_materialize_grads(False)
+        return weights, ids
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad_weights, _):
+        if grad_weights is None:
+            return None, None, None
+        logits, weights, ids = ctx.saved_tensors
+        return route_backward(grad_weights.contiguous(), logits, weights, ids, ctx.renormalise), None, None
+
+
+class DispatchFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, ids, n_experts):
+        rows, plan = dispatch_forward(x, ids, n_experts)
+        ctx.n_keys, ctx.tokens = plan.n_keys, x.shape[0]
+        ctx.save_for_backward(plan.position, plan.offsets)
+        ctx.set_materialize_grads(False)
+        if isinstance(ids, KeyOrder):
+            return rows
+        ctx.mark_non_differentiable(plan.order, plan.position, plan.offsets)
+        return rows, plan.order, plan.position, plan.offsets
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad_rows, *_):
+        if grad_rows is None:
+            return None, None, None
+        position, offsets = ctx.saved_tensors
+        plan = KeyOrder(position, position, offsets, ctx.n_keys)
+        k = position.numel() // ctx.tokens if ctx.tokens else 1
+        return dispatch_backward(_rows_apart(grad_rows), plan, k), None, None
+
+
+class CombineFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, rows, weights, plan, out_dtype):
+        ctx.plan = plan
+        ctx.save_for_backward(rows, weights)
+        ctx.set_materialize_grads(False)
+        return combine_forward(rows, weights, plan, out_dtype)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad_out):
+        if grad_out is None:
+            return None, None, None, None
+        rows, weights = ctx.saved_tensors
+        return *combine_backward(_rows_apart(grad_out), rows, weights, ctx.plan, *ctx.needs_input_grad[:2]), None, None
+
+
+class EmbedFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, table, ids, scale, out_dtype):
+        ctx.table_rows, ctx.dtype, ctx.scale = table.shape[0], table.dtype, scale
+        ctx.save_for_backward(ids)
+        ctx.set_materialize_grads(False)
+        return embed_forward(table, ids, scale, out_dtype)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad_out):
+        if grad_out is None:
+            return None, None, None, None
+        ids, = ctx.saved_tensors
+        grad_out = _rows_apart(grad_out) if ids.dim() == 1 else grad_out.contiguous()
+        return embed_backward(grad_out, ids, ctx.table_rows, ctx.scale, ctx.dtype), None, None, None
+
+
+def _rows_apart(g: torch.Tensor) -> torch.Tensor:
+    """A gradient whose rows the kernels can read (a sum's gradient has stride 0 within its rows)."""
+    return g if g.shape[-1] <= 1 or g.stride(-1) == 1 else g.contiguous()
+
+
+def route(logits: torch.Tensor, k: int, renormalise: bool = True):
+    """Differentiable route_forward: (weights, ids)."""
+    return RouteFunction.apply(logits, k, renormalise)
+
+
+def dispatch(x: torch.Tensor, ids, n_experts: int | None = None):
+    """Differentiable dispatch_forward: (rows, plan)."""
+    if isinstance(ids, KeyOrder):
+        return DispatchFunction.apply(x, ids, None), ids
+    rows, order, position, offsets = DispatchFunction.apply(x, ids, n_experts)
+    return rows, KeyOrder(order, position, offsets, n_experts)
+
+
+def combine(rows: torch.Tensor, weights: torch.Tensor, plan: KeyOrder, out_dtype=None) -> torch.Tensor:
+    """Differentiable combine_forward."""
+    return CombineFunction.apply(rows, weights, plan, out_dtype)
+
+
+def embed(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, out_dtype=None) -> torch.Tensor:
+    """Differentiable embed_forward; the table's gradient is dense."""
+    return EmbedFunction.apply(table, ids, scale, out_dtype)

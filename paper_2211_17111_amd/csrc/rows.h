@@ -24,9 +24,10 @@ struct SortLayout {
 };
 SortLayout sort_layout(int64_t n, int64_t n_keys);
 
+// position or sorted_keys (n_keys for a dropped slot) may be NULL.
 hipError_t launch_sort_keys(int64_t n, int64_t n_keys, int key_type, const void* keys,
-                            int32_t* order, int32_t* position, int32_t* offsets, void* workspace,
-                            hipStream_t stream);
+                            int32_t* order, int32_t* position, int32_t* offsets,
+                            int32_t* sorted_keys, void* workspace, hipStream_t stream);
 
 hipError_t launch_route_forward(int64_t rows, int32_t n_experts, int32_t k, int dtype,
                                 const void* logits, int64_t stride, bool renormalise,
@@ -56,8 +57,11 @@ hipError_t launch_embed_forward(int64_t n, int64_t table_rows, int64_t C, int in
                                 hipStream_t stream);
 struct EmbedLayout {
   size_t sort;                      // workspace of the sort
-  size_t order, position, offsets;  // int32[n], int32[n], int32[table_rows + 1]
+  size_t order, keys, offsets;  // int32[n], int32[n], int32[table_rows + 1]
+  size_t partials;              // float[2 * ranges][C]
   size_t total;
+  int64_t ranges;  // of RG sorted slots
+  int32_t RG;
 };
 EmbedLayout embed_layout(int64_t n, int64_t table_rows, int64_t C);
 hipError_t launch_embed_backward(int64_t n, int64_t table_rows, int64_t C, int in_dtype,

@@ -130,7 +130,7 @@ int bevpool_sort_keys(int64_t n, int64_t n_keys, int key_type, const void* keys,
   CHECK(check_workspace(workspace, workspace_bytes, bevpool::sort_layout(n, n_keys).total,
                         "sort_keys"));
   return from_hip(bevpool::launch_sort_keys(n, n_keys, key_type, keys, order, position, offsets,
-                                            workspace, static_cast<hipStream_t>(stream)),
+                                            nullptr, workspace, static_cast<hipStream_t>(stream)),
                   "bevpool_sort_keys");
 }
 
@@ -188,7 +188,7 @@ int bevpool_dispatch_forward(int64_t rows, int32_t k, int64_t C, int64_t n_keys,
                         "dispatch_forward"));
   hipStream_t s = static_cast<hipStream_t>(stream);
   CHECK(from_hip(bevpool::launch_sort_keys(rows * k, n_keys, key_type, ids, order, position,
-                                           offsets, workspace, s),
+                                           offsets, nullptr, workspace, s),
                  "bevpool_dispatch_forward"));
   return from_hip(bevpool::launch_dispatch_rows(rows, k, C, dtype, x, x_stride, position,
                                                 offsets + n_keys, out, s),

@@ -201,8 +201,8 @@ SortLayout sort_layout(int64_t n, int64_t n_keys) {
 }
 
 hipError_t launch_sort_keys(int64_t n, int64_t n_keys, int key_type, const void* keys,
-                            int32_t* order, int32_t* position, int32_t* offsets, void* workspace,
-                            hipStream_t stream) {
+                            int32_t* order, int32_t* position, int32_t* offsets,
+                            int32_t* sorted_keys, void* workspace, hipStream_t stream) {
   const unsigned ogrid = (unsigned)((n_keys + 1 + 255) / 256);
   if (n == 0) {
     k_zero_i32<<<ogrid, 256, 0, stream>>>(offsets, n_keys + 1);
@@ -221,7 +221,9 @@ hipError_t launch_sort_keys(int64_t n, int64_t n_keys, int key_type, const void*
   for (int p = 0; p < L.passes; ++p) {
     const int shift = p * L.digit_bits;
     const bool last = p == L.passes - 1;
-    int32_t* out_keys = L.passes > 1 ? W(L.keys[p & 1]) : nullptr;
+    int32_t* out_keys = last && sorted_keys != nullptr ? sorted_keys
+                        : L.passes > 1                ? W(L.keys[p & 1])
+                                                       : nullptr;
     int32_t* out_slots = last ? order : W(L.vals[p & 1]);
     int32_t* pos = last ? position : nullptr;
     int32_t* off = L.passes == 1 ? offsets : nullptr;

@@ -60,6 +60,19 @@ __device__ __forceinline__ void load_row(const T* p, int left, float (&v)[M]) {
   }
 }
 
+// The vector at p as it is, zeros past `left`, and v += its elements.
+template <typename T>
+__device__ __forceinline__ typename RowVec<T>::type load_raw(const T* p, int left) {
+  using V = typename RowVec<T>::type;
+  constexpr int N = RowVec<T>::N;
+  if (left >= N) return *reinterpret_cast<const V*>(p);
+  V t = {};
+#pragma unroll
+  for (int e = 0; e < N; ++e)
+    if (e < left) t[e] = p[e];
+  return t;
+}
+
 template <typename T, int M>
 __device__ __forceinline__ void store_row(T* p, int left, const float (&v)[M]) {
   constexpr int N = RowVec<T>::N < M ? RowVec<T>::N : M;  // (4 of a narrow type, from float32)

@@ -13,13 +13,13 @@ namespace bevpool {
 // Sort of n keys: `passes` radix passes of at most kSortBits bits over the
 // keys 0 .. n_keys (n_keys = dropped).
 constexpr int kSortBits = 10;
-constexpr int kSortTile = 2048;
+constexpr int kSortTile = 1024;
+constexpr int kSmallSort = 4096;  // most slots that one workgroup sorts
 struct SortLayout {
-  size_t hist;    // int32[tiles << digit_bits]: tile counts, digits together
-  size_t totals;  // int32[1 << digit_bits]
-  size_t keys[2], vals[2];  // int32[n] each, with several passes
-  size_t total;   // bytes
-  int64_t tiles;
+  size_t tile_counts, group_counts, totals;  // int32[digits] per tile, per group, in all
+  size_t keys[2], vals[2];                   // int32[n] each, with several passes
+  size_t total;                              // bytes
+  int64_t tiles, groups;
   int bits, passes, digit_bits;
 };
 SortLayout sort_layout(int64_t n, int64_t n_keys);

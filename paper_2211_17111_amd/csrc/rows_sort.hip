@@ -2,159 +2,268 @@
 // analogue of the plan's sort for keys that a model gives anew on every call.
 //
 // The keys 0 .. n_keys (n_keys = dropped) are sorted by radix passes of at
-// most 10 bits, so expert ids take one pass and the ids of a large table two:
-//   hist      the digit counts of every tile of 2048 slots
-//   scan      per digit, the counts of the tiles before each tile, and the total
-//   scatter   every slot to its digit's start (a scan of the totals), plus the
-//             earlier tiles' count, plus its rank in the tile
-// A slot's rank in its tile comes from wave ballots (one per digit bit finds
-// the lanes of equal digit) and counters per wave and digit, all in slot
-// order: the sort is stable and every result the same on every run.  The last
-// pass writes order and position.  With one pass the starts of the digits are
-// the offsets; else every key's offset is searched in the sorted keys.
+// most 10 bits, so expert ids take one pass and the ids of a large table two.
+// A slot's rank among the equal digits of its tile comes from wave ballots (one
+// per digit bit finds the lanes of equal digit) and counters per wave and digit,
+// all in slot order: the sort is stable and every result the same on every run.
+//
+// Up to 4096 slots one workgroup does all passes in LDS.  More slots are cut
+// into tiles of 1024, eight to a group, and every pass is
+//   hist      per group, the digit counts of its tiles, summed over the tiles
+//             before each, and the group's counts
+//   (scan     per digit, the sum over the groups before each group, and over
+//             all, where there are more than 32 groups)
+//   scatter   every slot to its digit's start, plus the count in earlier groups
+//             and tiles, plus its rank in the tile
+// The last pass writes order, position and the sorted keys.  With one pass the
+// starts of the digits are the offsets; else every key's offset is searched in
+// the sorted keys.
+//
+// Latency is what a call costs: the data of 131,072 slots is 1.5 MB.
+// Microseconds per sort, launches back to back in a graph, with 128 and with
+// 131,072 keys (two passes and the search):
+//   slots            64   1024   4096   8192  16384  131072  1000000
+//   128 keys        4.1    4.6    7.8    9.2    9.5    10.3     24.7
+//   131,072 keys    9.4   11.7   21.4   26.9   28.5    33.9     88.3
+// One workgroup takes 12.9 and 34.5 at 8192 slots, and tiles 8.6 and 24.5 at
+// 4097: hence the border at 4096.
 
 #include <algorithm>
 
 #include "device_utils.h"
 #include "rows.h"
+#include "rows_sort.h"
 #include "rows_vec.h"
 
 namespace bevpool {
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / kWave;
-constexpr int kRounds = kSortTile / kThreads;  // 64-slot rounds of a wave
-constexpr int kWaveSpan = kRounds * kWave;     // slots of a wave, consecutive
-constexpr int kMaxDigits = 1 << kSortBits;
+constexpr int kGroupTiles = 8;
+constexpr int kGroup = kSortTile * kGroupTiles;  // slots of a hist block
+constexpr int kFusedGroups = 32;                 // most groups that a scatter block adds up itself
 
 __global__ __launch_bounds__(256) void k_zero_i32(int32_t* __restrict__ a, int64_t n) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i < n) a[i] = 0;
 }
 
+// tile_counts[tile][digit]: the digit's count in the earlier tiles of the
+// group; group_counts[group][digit]: in the whole group.
 template <typename TKey>
-__global__ __launch_bounds__(kThreads) void k_keys_hist(const TKey* __restrict__ keys, int64_t n,
-                                                        int32_t n_keys, int shift, int digit_bits,
-                                                        int32_t* __restrict__ hist) {
-  __shared__ int h[kMaxDigits];
+__global__ __launch_bounds__(kSortTile) void k_keys_hist(const TKey* __restrict__ keys, int64_t n,
+                                                         int32_t n_keys, int shift, int digit_bits,
+                                                         int32_t* __restrict__ tile_counts,
+                                                         int32_t* __restrict__ group_counts) {
+  __shared__ int h[kGroupTiles][kMaxDigits];
   const int digits = 1 << digit_bits;
-  for (int i = threadIdx.x; i < digits; i += kThreads) h[i] = 0;
-  __syncthreads();
-  const int64_t base = (int64_t)blockIdx.x * kSortTile;
+  const int64_t base = (int64_t)blockIdx.x * kGroup;
+  const int t = threadIdx.x;
+  int32_t key[kGroupTiles];
 #pragma unroll
-  for (int r = 0; r < kRounds; ++r) {
-    const int64_t i = base + r * kThreads + threadIdx.x;
-    if (i < n) atomicAdd(&h[(key_or_drop(keys, i, n_keys) >> shift) & (digits - 1)], 1);
+  for (int k = 0; k < kGroupTiles; ++k) {
+    const int64_t i = base + k * kSortTile + t;
+    key[k] = i < n ? key_or_drop(keys, i, n_keys) : -1;
   }
-  __syncthreads();
-  for (int i = threadIdx.x; i < digits; i += kThreads)
-    hist[(int64_t)blockIdx.x * digits + i] = h[i];
+  for (int i = t; i < kGroupTiles * kMaxDigits; i += kSortTile) (&h[0][0])[i] = 0;
+  lds_barrier();
+#pragma unroll
+  for (int k = 0; k < kGroupTiles; ++k)
+    if (key[k] >= 0) atomicAdd(&h[k][(key[k] >> shift) & (digits - 1)], 1);
+  lds_barrier();
+  if (t < digits) {
+    int sum = 0;
+#pragma unroll
+    for (int k = 0; k < kGroupTiles; ++k) {
+      tile_counts[((int64_t)blockIdx.x * kGroupTiles + k) * digits + t] = sum;
+      sum += h[k][t];
+    }
+    group_counts[(int64_t)blockIdx.x * digits + t] = sum;
+  }
 }
 
-// One digit per thread; hist becomes the exclusive prefix over the tiles.
-__global__ __launch_bounds__(kWave) void k_keys_scan(int32_t* __restrict__ hist, int64_t tiles,
-                                                     int digits, int32_t* __restrict__ totals) {
+// One digit per thread; group_counts becomes the exclusive sum over the groups.
+__global__ __launch_bounds__(kWave) void k_keys_scan(int32_t* __restrict__ group_counts,
+                                                     int64_t groups, int digits,
+                                                     int32_t* __restrict__ totals) {
   const int d = blockIdx.x * kWave + threadIdx.x;
   if (d >= digits) return;
   int sum = 0;
-  constexpr int kBatch = 8;  // loads in flight
-  int64_t t = 0;
-  for (; t + kBatch <= tiles; t += kBatch) {
+  constexpr int kBatch = 16;  // loads in flight
+  for (int64_t g = 0; g < groups; g += kBatch) {
     int32_t c[kBatch];
 #pragma unroll
-    for (int u = 0; u < kBatch; ++u) c[u] = hist[(t + u) * digits + d];
+    for (int u = 0; u < kBatch; ++u) c[u] = g + u < groups ? group_counts[(g + u) * digits + d] : 0;
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
-      hist[(t + u) * digits + d] = sum;
+      if (g + u < groups) group_counts[(g + u) * digits + d] = sum;
       sum += c[u];
     }
-  }
-  for (; t < tiles; ++t) {
-    const int32_t c = hist[t * digits + d];
-    hist[t * digits + d] = sum;
-    sum += c;
   }
   totals[d] = sum;
 }
 
-// `slots` NULL: the slot is the key's index (first pass).  The last pass sets
-// order and position, the others keys_out and slots_out; keys_out is also set
-// in a last pass whose sorted keys are searched for the offsets.  offsets is
-// set in an only pass.
+// `slots` NULL: the slot is the key's index (first pass).  totals NULL: the
+// groups' counts have not been summed.  position, keys_out and offsets may be
+// NULL.
 template <typename TKey>
-__global__ __launch_bounds__(kThreads) void k_keys_scatter(
+__global__ __launch_bounds__(kTileThreads) void k_keys_scatter(
     const TKey* __restrict__ keys, const int32_t* __restrict__ slots, int64_t n, int32_t n_keys,
-    int shift, int digit_bits, const int32_t* __restrict__ hist, const int32_t* __restrict__ totals,
+    int shift, int digit_bits, const int32_t* __restrict__ tile_counts,
+    const int32_t* __restrict__ group_counts, const int32_t* __restrict__ totals, int groups,
     int32_t* __restrict__ keys_out, int32_t* __restrict__ slots_out,
     int32_t* __restrict__ position, int32_t* __restrict__ offsets) {
-  __shared__ int cnt[kWaves][kMaxDigits];
-  __shared__ int s_scan[kWaves];
+  __shared__ int cnt[kTileWaves][kMaxDigits];
+  __shared__ int s_scan[kTileWaves];
   const int digits = 1 << digit_bits;
-  for (int w = 0; w < kWaves; ++w)
-    for (int i = threadIdx.x; i < digits; i += kThreads) cnt[w][i] = 0;
-  __syncthreads();
-
-  const int lane = lane_id();
-  const int wid = threadIdx.x / kWave;
-  const int64_t base = (int64_t)blockIdx.x * kSortTile + (int64_t)wid * kWaveSpan;
-  int32_t key[kRounds], rank[kRounds];
+  const int64_t base = (int64_t)blockIdx.x * kSortTile;
+  const int n_tile = (int)min<int64_t>(kSortTile, n - base);
+  int32_t key[kTileRounds], slot[kTileRounds], rank[kTileRounds];
 #pragma unroll
-  for (int r = 0; r < kRounds; ++r) {
-    const int64_t i = base + r * kWave + lane;
-    const bool valid = i < n;
-    key[r] = valid ? key_or_drop(keys, i, n_keys) : 0;
-    const int digit = (key[r] >> shift) & (digits - 1);
-    uint64_t same = wave_ballot(valid);
-    for (int b = 0; b < digit_bits; ++b) {
-      const bool bit = (digit >> b) & 1;
-      const uint64_t m = wave_ballot(bit);
-      same &= bit ? m : ~m;
-    }
-    const int below = rank_below(same);
-    const int prior = cnt[wid][digit];
-    if (valid && below == 0) cnt[wid][digit] = prior + __popcll(same);
-    rank[r] = prior + below;
+  for (int r = 0; r < kTileRounds; ++r) {
+    const int i = tile_index(r);
+    key[r] = i < n_tile ? key_or_drop(keys, base + i, n_keys) : 0;
+    slot[r] = i < n_tile ? (slots != nullptr ? slots[base + i] : (int32_t)(base + i)) : 0;
   }
-  __syncthreads();
-  // starts of the digits: thread t scans digits [t * per, (t + 1) * per)
-  constexpr int kPer = kMaxDigits / kThreads;
-  int tot[kPer];
+  // this thread's digits t per .. t per + per - 1: their counts in all slots
+  // and in the earlier groups and tiles
+  const int per = max(1, digits / kTileThreads);
+  const int mine = blockIdx.x / kGroupTiles;
+  int tot[kDigitsPerThread], before[kDigitsPerThread];
+#pragma unroll
+  for (int q = 0; q < kDigitsPerThread; ++q) {
+    const int d = threadIdx.x * per + q;
+    tot[q] = before[q] = 0;
+    if (q >= per || d >= digits) continue;
+    before[q] = tile_counts[(int64_t)blockIdx.x * digits + d];
+    if (totals != nullptr) {
+      tot[q] = totals[d];
+      before[q] += group_counts[(int64_t)mine * digits + d];
+    } else {
+#pragma unroll 8
+      for (int g = 0; g < groups; ++g) {
+        const int c = group_counts[(int64_t)g * digits + d];
+        tot[q] += c;
+        before[q] += g < mine ? c : 0;
+      }
+    }
+  }
+  tile_ranks(key, n_tile, shift, digit_bits, cnt, rank);
   int sum = 0;
 #pragma unroll
-  for (int q = 0; q < kPer; ++q) {
-    const int d = threadIdx.x * kPer + q;
-    tot[q] = d < digits ? totals[d] : 0;
-    sum += tot[q];
-  }
+  for (int q = 0; q < kDigitsPerThread; ++q) sum += tot[q];
   int all;
-  int start = block_exclusive_scan<kThreads>(sum, s_scan, &all);
+  int start = block_exclusive_scan<kTileThreads, true>(sum, s_scan, &all);
 #pragma unroll
-  for (int q = 0; q < kPer; ++q) {
-    const int d = threadIdx.x * kPer + q;
-    if (d < digits) {
-      int at = start + hist[(int64_t)blockIdx.x * digits + d];
+  for (int q = 0; q < kDigitsPerThread; ++q) {
+    const int d = threadIdx.x * per + q;
+    if (q >= per || d >= digits) continue;
+    int at = start + before[q];
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        const int c = cnt[w][d];
-        cnt[w][d] = at;
-        at += c;
-      }
-      if (offsets != nullptr && blockIdx.x == 0 && d <= n_keys) offsets[d] = start;
+    for (int w = 0; w < kTileWaves; ++w) {
+      const int c = cnt[w][d];
+      cnt[w][d] = at;
+      at += c;
     }
+    if (offsets != nullptr && blockIdx.x == 0 && d <= n_keys) offsets[d] = start;
     start += tot[q];
   }
-  __syncthreads();
+  lds_barrier();
 #pragma unroll
-  for (int r = 0; r < kRounds; ++r) {
-    const int64_t i = base + r * kWave + lane;
-    if (i >= n) continue;
-    const int32_t pos = cnt[wid][(key[r] >> shift) & (digits - 1)] + rank[r];
-    const int32_t slot = slots != nullptr ? slots[i] : (int32_t)i;
-    slots_out[pos] = slot;
+  for (int r = 0; r < kTileRounds; ++r) {
+    if (tile_index(r) >= n_tile) continue;
+    const int32_t pos = cnt[threadIdx.x / kWave][(key[r] >> shift) & (digits - 1)] + rank[r];
+    slots_out[pos] = slot[r];
     if (keys_out != nullptr) keys_out[pos] = key[r];
-    if (position != nullptr) position[slot] = pos;
+    if (position != nullptr) position[slot[r]] = pos;
+  }
+}
+
+// All passes over at most kSmallSort slots in one workgroup.
+constexpr int kSmallThreads = 1024;
+constexpr int kSmallWaves = kSmallThreads / kWave;
+constexpr int kSmallRounds = kSmallSort / kSmallThreads;
+
+template <typename TKey>
+__global__ __launch_bounds__(kSmallThreads) void k_keys_small(
+    const TKey* __restrict__ keys, int32_t n, int32_t n_keys, int passes, int digit_bits,
+    int32_t* __restrict__ order, int32_t* __restrict__ position, int32_t* __restrict__ offsets,
+    int32_t* __restrict__ sorted_keys) {
+  __shared__ uint16_t cnt[kSmallWaves][kMaxDigits];  // (a wave has at most 256 slots)
+  __shared__ int32_t s_start[kMaxDigits];
+  __shared__ int s_scan[kSmallWaves];
+  __shared__ int32_t s_key[kSmallSort];
+  __shared__ uint16_t s_slot[kSmallSort];
+  const int t = threadIdx.x;
+  const int wid = t / kWave, lane = t % kWave;
+  const int digits = 1 << digit_bits;
+  const int rounds = (n + kSmallThreads - 1) / kSmallThreads;
+  const int base = wid * rounds * kWave + lane;  // the wave's slots are consecutive
+  int32_t key[kSmallRounds];
+  uint32_t slot[kSmallRounds];
+#pragma unroll
+  for (int r = 0; r < kSmallRounds; ++r) {
+    const int i = base + r * kWave;
+    const bool on = r < rounds && i < n;
+    key[r] = on ? key_or_drop(keys, i, n_keys) : 0;
+    slot[r] = (uint32_t)i;
+  }
+  for (int p = 0; p < passes; ++p) {
+    const int shift = p * digit_bits;
+    for (int w = 0; w < kSmallWaves; ++w)
+      for (int d = t; d < digits; d += kSmallThreads) cnt[w][d] = 0;
+    lds_barrier();
+    if (p > 0) {
+#pragma unroll
+      for (int r = 0; r < kSmallRounds; ++r) {
+        const int i = base + r * kWave;
+        if (r >= rounds || i >= n) continue;
+        key[r] = s_key[i];
+        slot[r] = s_slot[i];
+      }
+    }
+    int32_t rank[kSmallRounds];
+#pragma unroll
+    for (int r = 0; r < kSmallRounds; ++r) {
+      rank[r] = 0;
+      if (r >= rounds) continue;  // (uniform)
+      const bool on = base + r * kWave < n;
+      const int digit = (key[r] >> shift) & (digits - 1);
+      const uint64_t same = same_digit(digit, on, digit_bits);
+      const int below = rank_below(same);
+      const int prior = cnt[wid][digit];
+      if (on && below == 0) cnt[wid][digit] = (uint16_t)(prior + __popcll(same));
+      rank[r] = prior + below;
+    }
+    lds_barrier();
+    int tot = 0;  // digit t: the waves' offsets within the digit, and its count
+    if (t < digits)
+      for (int w = 0; w < kSmallWaves; ++w) {
+        const int c = cnt[w][t];
+        cnt[w][t] = (uint16_t)tot;
+        tot += c;
+      }
+    int all;
+    const int start = block_exclusive_scan<kSmallThreads, true>(tot, s_scan, &all);
+    if (t < digits) s_start[t] = start;
+    if (passes == 1 && t <= n_keys && t < digits) offsets[t] = start;
+    lds_barrier();
+    const bool last = p == passes - 1;
+#pragma unroll
+    for (int r = 0; r < kSmallRounds; ++r) {
+      if (r >= rounds || base + r * kWave >= n) continue;
+      const int digit = (key[r] >> shift) & (digits - 1);
+      const int pos = s_start[digit] + cnt[wid][digit] + rank[r];
+      if (last) {
+        order[pos] = (int32_t)slot[r];
+        if (position != nullptr) position[slot[r]] = pos;
+        if (sorted_keys != nullptr) sorted_keys[pos] = key[r];
+      } else {
+        s_key[pos] = key[r];
+        s_slot[pos] = (uint16_t)slot[r];
+      }
+    }
+    lds_barrier();
   }
 }
 
@@ -181,20 +290,24 @@ SortLayout sort_layout(int64_t n, int64_t n_keys) {
   L.passes = (L.bits + kSortBits - 1) / kSortBits;
   L.digit_bits = (L.bits + L.passes - 1) / L.passes;
   L.tiles = (n + kSortTile - 1) / kSortTile;
+  L.groups = (n + kGroup - 1) / kGroup;
   size_t off = 0;
   auto take = [&](int64_t ints) {
     const size_t o = off;
     off += (sizeof(int32_t) * (size_t)ints + 255) & ~size_t(255);
     return o;
   };
-  if (n > 0) {
-    L.hist = take(L.tiles << L.digit_bits);
+  if (n > kSmallSort) {
+    L.tile_counts = take((L.groups * kGroupTiles) << L.digit_bits);
+    L.group_counts = take(L.groups << L.digit_bits);
     L.totals = take(int64_t(1) << L.digit_bits);
     if (L.passes > 1)
       for (int i = 0; i < 2; ++i) {
         L.keys[i] = take(n);
         L.vals[i] = take(n);
       }
+  } else if (n > 0 && L.passes > 1) {
+    L.keys[0] = take(n);  // (sorted, for the offsets)
   }
   L.total = off;
   return L;
@@ -211,11 +324,21 @@ hipError_t launch_sort_keys(int64_t n, int64_t n_keys, int key_type, const void*
   const SortLayout L = sort_layout(n, n_keys);
   char* ws = static_cast<char*>(workspace);
   auto W = [&](size_t o) { return reinterpret_cast<int32_t*>(ws + o); };
-  int32_t *hist = W(L.hist), *totals = W(L.totals);
   const int32_t nk = (int32_t)n_keys;
+  if (n <= kSmallSort) {
+    int32_t* sorted = sorted_keys != nullptr ? sorted_keys : L.passes > 1 ? W(L.keys[0]) : nullptr;
+    auto go = [&](auto* k) {
+      k_keys_small<<<1, kSmallThreads, 0, stream>>>(k, (int32_t)n, nk, L.passes, L.digit_bits,
+                                                    order, position, offsets, sorted);
+    };
+    if (key_type == BEVPOOL_KEY_I64) go(static_cast<const int64_t*>(keys));
+    else go(static_cast<const int32_t*>(keys));
+    if (L.passes > 1) k_keys_offsets<<<ogrid, 256, 0, stream>>>(sorted, n, nk, offsets);
+    return hipGetLastError();
+  }
+  int32_t *tile_counts = W(L.tile_counts), *group_counts = W(L.group_counts);
+  int32_t* totals = L.groups > kFusedGroups ? W(L.totals) : nullptr;
   const int digits = 1 << L.digit_bits;
-  const dim3 grid((unsigned)L.tiles);
-  const unsigned sgrid = (unsigned)((digits + kWave - 1) / kWave);
   const int32_t* in_keys = nullptr;
   const int32_t* in_slots = nullptr;
   for (int p = 0; p < L.passes; ++p) {
@@ -228,10 +351,14 @@ hipError_t launch_sort_keys(int64_t n, int64_t n_keys, int key_type, const void*
     int32_t* pos = last ? position : nullptr;
     int32_t* off = L.passes == 1 ? offsets : nullptr;
     auto pass = [&](auto* k) {
-      k_keys_hist<<<grid, kThreads, 0, stream>>>(k, n, nk, shift, L.digit_bits, hist);
-      k_keys_scan<<<sgrid, kWave, 0, stream>>>(hist, L.tiles, digits, totals);
-      k_keys_scatter<<<grid, kThreads, 0, stream>>>(k, in_slots, n, nk, shift, L.digit_bits, hist,
-                                                    totals, out_keys, out_slots, pos, off);
+      k_keys_hist<<<(unsigned)L.groups, kSortTile, 0, stream>>>(k, n, nk, shift, L.digit_bits,
+                                                                tile_counts, group_counts);
+      if (totals != nullptr)
+        k_keys_scan<<<(unsigned)((digits + kWave - 1) / kWave), kWave, 0, stream>>>(
+            group_counts, L.groups, digits, totals);
+      k_keys_scatter<<<(unsigned)L.tiles, kTileThreads, 0, stream>>>(
+          k, in_slots, n, nk, shift, L.digit_bits, tile_counts, group_counts, totals,
+          (int)L.groups, out_keys, out_slots, pos, off);
     };
     if (p > 0)
       pass(in_keys);

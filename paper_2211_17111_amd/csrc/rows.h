@@ -37,6 +37,10 @@ hipError_t launch_route_backward(int64_t rows, int32_t n_experts, int32_t k, int
                                  const float* weights, const int32_t* ids, bool renormalise,
                                  void* grad_logits, hipStream_t stream);
 
+hipError_t launch_dispatch_forward(int64_t rows, int32_t k, int64_t C, int64_t n_keys, int dtype,
+                                   const void* x, int64_t x_stride, int key_type, const void* ids,
+                                   int32_t* order, int32_t* position, int32_t* offsets, void* out,
+                                   void* workspace, hipStream_t stream);
 hipError_t launch_dispatch_rows(int64_t rows, int32_t k, int64_t C, int dtype, const void* x,
                                 int64_t x_stride, const int32_t* position, const int32_t* kept,
                                 void* out, hipStream_t stream);

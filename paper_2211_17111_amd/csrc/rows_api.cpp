@@ -186,12 +186,9 @@ int bevpool_dispatch_forward(int64_t rows, int32_t k, int64_t C, int64_t n_keys,
   REQUIRE_PTR(offsets);
   CHECK(check_workspace(workspace, workspace_bytes, bevpool::sort_layout(rows * k, n_keys).total,
                         "dispatch_forward"));
-  hipStream_t s = static_cast<hipStream_t>(stream);
-  CHECK(from_hip(bevpool::launch_sort_keys(rows * k, n_keys, key_type, ids, order, position,
-                                           offsets, nullptr, workspace, s),
-                 "bevpool_dispatch_forward"));
-  return from_hip(bevpool::launch_dispatch_rows(rows, k, C, dtype, x, x_stride, position,
-                                                offsets + n_keys, out, s),
+  return from_hip(bevpool::launch_dispatch_forward(rows, k, C, n_keys, dtype, x, x_stride, key_type,
+                                                   ids, order, position, offsets, out, workspace,
+                                                   static_cast<hipStream_t>(stream)),
                   "bevpool_dispatch_forward");
 }
 

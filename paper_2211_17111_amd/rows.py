@@ -26,6 +26,7 @@ have to be ready on.  No call synchronises or reads back.
 from __future__ import annotations
 
 import ctypes
+import functools
 from dataclasses import dataclass
 
 import torch
@@ -80,10 +81,16 @@ def _call(name: str, *args) -> None:
         _bp._check(lib, status, name)
 
 
+@functools.lru_cache(maxsize=1024)
 def _size(name: str, *args) -> int:
     n = _sz(0)
     _call(name, *args, ctypes.byref(n))
     return n.value
+
+
+def _stream(dev: torch.device) -> int:
+    """Handle of dev's current stream (torch's raw query costs a tenth of a stream object)."""
+    return _bp._raw_stream(dev.index) if _bp._raw_stream else torch.cuda.current_stream(dev).cuda_stream
 
 
 # ----------------------------------------------------------------- arguments
@@ -155,10 +162,11 @@ class KeyOrder:
 
 
 def _key_order(n: int, n_keys: int, dev: torch.device):
-    i32 = dict(dtype=torch.int32, device=dev)
-    plan = KeyOrder(torch.empty(n, **i32), torch.empty(n, **i32), torch.empty(n_keys + 1, **i32), n_keys)
     nbytes = _size("bevpool_sort_keys_workspace_size", n, n_keys)
-    return plan, torch.empty(nbytes, dtype=torch.uint8, device=dev), nbytes
+    i32 = torch.int32
+    plan = KeyOrder(torch.empty(n, dtype=i32, device=dev), torch.empty(n, dtype=i32, device=dev),
+                    torch.empty(n_keys + 1, dtype=i32, device=dev), n_keys)
+    return plan, torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None, nbytes
 
 
 # --------------------------------------------------------------- key sorting
@@ -175,7 +183,7 @@ def sort_keys(keys: torch.Tensor, n_keys: int, stream=None) -> KeyOrder:
     n = keys.numel()
     plan, ws, nbytes = _key_order(n, n_keys, dev)
     _call("bevpool_sort_keys", n, n_keys, _KEY_CODE[keys.dtype], keys.data_ptr(), plan.order.data_ptr(),
-          plan.position.data_ptr(), plan.offsets.data_ptr(), ws.data_ptr(), nbytes, _bp._stream(None))
+          plan.position.data_ptr(), plan.offsets.data_ptr(), _bp._ptr(ws), nbytes, _stream(dev))
     return plan
 
 
@@ -196,7 +204,7 @@ def route_forward(logits: torch.Tensor, k: int, renormalise: bool = True, stream
     weights = torch.empty((T, k), dtype=torch.float32, device=dev)
     ids = torch.empty((T, k), dtype=torch.int32, device=dev)
     _call("bevpool_route_forward", T, E, k, _DTYPE_CODE[logits.dtype], logits.data_ptr(), stride, int(renormalise),
-          weights.data_ptr(), ids.data_ptr(), _bp._stream(None))
+          weights.data_ptr(), ids.data_ptr(), _stream(dev))
     return weights, ids
 
 
@@ -216,7 +224,7 @@ def route_backward(grad_weights: torch.Tensor, logits: torch.Tensor, weights: to
             return route_backward(grad_weights, logits, weights, ids, renormalise)
     grad = torch.empty((T, E), dtype=logits.dtype, device=dev)
     _call("bevpool_route_backward", T, E, k, _DTYPE_CODE[logits.dtype], grad_weights.data_ptr(), logits.data_ptr(),
-          stride, weights.data_ptr(), ids.data_ptr(), int(renormalise), grad.data_ptr(), _bp._stream(None))
+          stride, weights.data_ptr(), ids.data_ptr(), int(renormalise), grad.data_ptr(), _stream(dev))
     return grad
 
 
@@ -250,12 +258,12 @@ def dispatch_forward(x: torch.Tensor, ids, n_experts: int | None = None, stream=
     out = torch.empty((n, C), dtype=x.dtype, device=dev)
     if plan is not None:
         _call("bevpool_dispatch_rows", T, k, C, _DTYPE_CODE[x.dtype], x.data_ptr(), stride, plan.position.data_ptr(),
-              kept, out.data_ptr(), _bp._stream(None))
+              kept, out.data_ptr(), _stream(dev))
         return out, plan
     plan, ws, nbytes = _key_order(n, n_experts, dev)
     _call("bevpool_dispatch_forward", T, k, C, n_experts, _DTYPE_CODE[x.dtype], x.data_ptr(), stride,
           _KEY_CODE[ids.dtype], ids.data_ptr(), plan.order.data_ptr(), plan.position.data_ptr(),
-          plan.offsets.data_ptr(), out.data_ptr(), ws.data_ptr(), nbytes, _bp._stream(None))
+          plan.offsets.data_ptr(), out.data_ptr(), _bp._ptr(ws), nbytes, _stream(dev))
     return out, plan
 
 
@@ -278,7 +286,7 @@ def dispatch_backward(grad_rows: torch.Tensor, plan: KeyOrder, k: int, stream=No
     C = grad_rows.shape[1]
     grad = torch.empty((T, C), dtype=grad_rows.dtype, device=dev)
     _call("bevpool_dispatch_backward", T, k, C, _DTYPE_CODE[grad_rows.dtype], grad_rows.data_ptr(), stride,
-          plan.position.data_ptr(), kept, grad.data_ptr(), _bp._stream(None))
+          plan.position.data_ptr(), kept, grad.data_ptr(), _stream(dev))
     return grad
 
 
@@ -305,7 +313,7 @@ def combine_forward(rows: torch.Tensor, weights: torch.Tensor, plan: KeyOrder, o
     out = torch.empty((T, C), dtype=odt, device=dev)
     _call("bevpool_combine_forward", T, k, C, _DTYPE_CODE[rows.dtype], _DTYPE_CODE[odt], _DTYPE_CODE[weights.dtype],
           rows.data_ptr(), stride, weights.data_ptr(), plan.position.data_ptr(), kept, out.data_ptr(),
-          _bp._stream(None))
+          _stream(dev))
     return out
 
 
@@ -333,7 +341,7 @@ def combine_backward(grad_out: torch.Tensor, rows: torch.Tensor, weights: torch.
     _call("bevpool_combine_backward", T, k, C, _DTYPE_CODE[rows.dtype], _DTYPE_CODE[grad_out.dtype],
           _DTYPE_CODE[weights.dtype], grad_out.data_ptr(), grad_stride, rows.data_ptr(), stride, weights.data_ptr(),
           plan.position.data_ptr(), kept, grad_rows.data_ptr() if need_rows else None,
-          grad_weights.data_ptr() if need_weights else None, _bp._stream(None))
+          grad_weights.data_ptr() if need_weights else None, _stream(dev))
     return grad_rows, grad_weights
 
 
@@ -356,7 +364,7 @@ def embed_forward(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, ou
     V, C = table.shape
     out = torch.empty(ids.shape + (C,), dtype=odt, device=dev)
     _call("bevpool_embed_forward", ids.numel(), V, C, _DTYPE_CODE[table.dtype], _DTYPE_CODE[odt], table.data_ptr(),
-          stride, _KEY_CODE[ids.dtype], ids.data_ptr(), scale, out.data_ptr(), _bp._stream(None))
+          stride, _KEY_CODE[ids.dtype], ids.data_ptr(), scale, out.data_ptr(), _stream(dev))
     return out
 
 
@@ -388,7 +396,7 @@ def embed_backward(grad_out: torch.Tensor, ids: torch.Tensor, table_rows: int, s
     ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
     _call("bevpool_embed_backward", n, table_rows, C, _DTYPE_CODE[grad_out.dtype], _DTYPE_CODE[gdt],
           grad_out.data_ptr(), stride, _KEY_CODE[ids.dtype], ids.data_ptr(), scale, grad.data_ptr(), ws.data_ptr(),
-          nbytes, _bp._stream(None))
+          nbytes, _stream(dev))
     return grad
 
 

@@ -62,7 +62,7 @@ struct Ranges {
 
 constexpr int kInFlight = 8;  // rows a lane group has in flight
 
-template <typename T, typename TO>
+template <typename T, typename TO, bool STREAM>
 __global__ __launch_bounds__(kRowThreads) void k_embed_ranges(const T* __restrict__ grad_out,
                                                               int64_t stride, Ranges a, int32_t W,
                                                               int32_t tiles, float scale,
@@ -76,12 +76,14 @@ __global__ __launch_bounds__(kRowThreads) void k_embed_ranges(const T* __restric
   const int64_t item = (int64_t)blockIdx.x * G + group;
   const int64_t r = item / tiles;
   if (r >= a.ranges) return;
-  const int c = ((int)(item - r * tiles) * W + threadIdx.x - group * W) * N;
+  const int vec = (int)(item - r * tiles) * W + threadIdx.x - group * W;
+  if (vec * N >= a.C) return;
+  const int c = vector_start<N>(vec, a.C);
   const int left = a.C - c;
   const int32_t kept = a.offsets[a.n_keys];
   const int64_t p0 = r * a.RG;
   const int32_t m = (int32_t)min<int64_t>(a.RG, kept - p0);  // (<= 0 behind the kept slots)
-  if (m <= 0 || left <= 0) return;
+  if (m <= 0) return;
   const int32_t before = p0 > 0 ? a.keys[p0 - 1] : -1;
   const int32_t after = p0 + m < kept ? a.keys[p0 + m] : -1;
   const int32_t* order = a.order + p0;
@@ -109,7 +111,7 @@ __global__ __launch_bounds__(kRowThreads) void k_embed_ranges(const T* __restric
     for (int u = 0; u < kInFlight; ++u) {
       const int32_t q = min(q0 + u, m - 1);  // (a repeat past the end, not added)
       key[u] = keys[q];
-      g[u] = load_raw<T>(grad_out + order[q] * stride + c, left);
+      g[u] = load_raw<T, STREAM>(grad_out + order[q] * stride + c, left);
     }
 #pragma unroll
     for (int u = 0; u < kInFlight; ++u) {
@@ -140,9 +142,10 @@ __global__ __launch_bounds__(kRowThreads) void k_embed_rest(RowSplit s, Ranges a
       const int32_t items = (int32_t)min<int64_t>(s.R, s.rows - row0) * s.cvb;
       for (uint32_t i = threadIdx.x; i < (uint32_t)items; i += kRowThreads) {
         const uint32_t q = s.by.div(i);
-        const int32_t c = (c0 + (int32_t)(i - q * (uint32_t)s.cvb)) * N;
+        const int32_t vec = c0 + (int32_t)(i - q * (uint32_t)s.cvb);
+        const int32_t c = vector_start<N>(vec, s.C);
         const int64_t v = row0 + q;
-        if (c < s.C && a.offsets[v] == a.offsets[v + 1])
+        if (vec < s.cv && a.offsets[v] == a.offsets[v + 1])
           store_row<TO>(grad_table + v * s.C + c, s.C - c, zero);
       }
     }
@@ -165,7 +168,7 @@ __global__ __launch_bounds__(kRowThreads) void k_embed_rest(RowSplit s, Ranges a
   const int W = min(kWave, cv - first_vec);
   const int G = kRowThreads / W;
   const int group = threadIdx.x / W;
-  const int c = (first_vec + threadIdx.x - group * W) * N;
+  const int c = vector_start<N>(first_vec + threadIdx.x - group * W, a.C);
   float acc[N] = {};
   if (group < G) {
     // the id's partial of range r + j: the second in the range where it starts
@@ -285,9 +288,13 @@ hipError_t launch_embed_backward(int64_t n, int64_t table_rows, int64_t C, int i
       const int64_t tiles = (cv + kWave - 1) / kWave;
       const int32_t W = (int32_t)((cv + tiles - 1) / tiles);
       const int64_t G = kRowThreads / W;
-      k_embed_ranges<T, TO>
-          <<<(unsigned)((L.ranges * tiles + G - 1) / G), kRowThreads, 0, stream>>>(
-              static_cast<const T*>(grad_out), grad_stride, a, W, (int32_t)tiles, scale, out);
+      auto go = [&](auto stream_hint) {
+        k_embed_ranges<T, TO, stream_hint.value>
+            <<<(unsigned)((L.ranges * tiles + G - 1) / G), kRowThreads, 0, stream>>>(
+                static_cast<const T*>(grad_out), grad_stride, a, W, (int32_t)tiles, scale, out);
+      };
+      if (stream_rows(n, C, sizeof(T))) go(std::true_type{});
+      else go(std::false_type{});
     }
     const RowSplit s = row_split(table_rows, C, RowVec<TO>::N);
     const int64_t parts = (s.cv + s.cvb - 1) / s.cvb;

@@ -14,6 +14,8 @@ namespace bevpool {
 
 namespace {
 
+constexpr int kSlots = 4;  // slots of a token whose places or rows a thread has in flight
+
 // Stores vector c of token t's row at the places of its k slots (`place` gives
 // them by slot), zeros for dropped ones.  The elements are moved as they are
 // (T: an unsigned integer of their size).
@@ -32,17 +34,22 @@ __device__ __forceinline__ void move_vector(const T* __restrict__ x, int64_t x_s
     for (int e = 0; e < N; ++e)
       if (e < left) v[e] = p[e];
   }
-  for (int j = 0; j < k; ++j) {
-    const int32_t pos = place(t * k + j);
-    if (pos < 0 || pos >= n) continue;
-    const V w = pos < kept ? v : V{};
-    T* q = out + (int64_t)pos * s.C + c;
-    if (left >= N) {
-      *reinterpret_cast<V*>(q) = w;
-    } else {
+  for (int j0 = 0; j0 < k; j0 += kSlots) {
+    int32_t pos[kSlots];
 #pragma unroll
-      for (int e = 0; e < N; ++e)
-        if (e < left) q[e] = w[e];
+    for (int u = 0; u < kSlots; ++u) pos[u] = j0 + u < k ? place(t * k + j0 + u) : -1;
+#pragma unroll
+    for (int u = 0; u < kSlots; ++u) {
+      if (pos[u] < 0 || pos[u] >= n) continue;
+      const V w = pos[u] < kept ? v : V{};
+      T* q = out + (int64_t)pos[u] * s.C + c;
+      if (left >= N) {
+        *reinterpret_cast<V*>(q) = w;
+      } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          if (e < left) q[e] = w[e];
+      }
     }
   }
 }
@@ -142,7 +149,7 @@ __device__ __forceinline__ float weight_at(const void* w, bool f32, int64_t i) {
 
 // out[t] = sum over kept j of w[t k + j] * in[position[t k + j]], w = 1 where
 // weights is NULL.
-template <typename T, typename TO>
+template <typename T, typename TO, bool STREAM>
 __global__ __launch_bounds__(kRowThreads) void k_combine(const T* __restrict__ in, int64_t stride,
                                                          RowSplit s, int k,
                                                          const void* __restrict__ weights,
@@ -150,6 +157,7 @@ __global__ __launch_bounds__(kRowThreads) void k_combine(const T* __restrict__ i
                                                          const int32_t* __restrict__ position,
                                                          const int32_t* __restrict__ kept_ptr,
                                                          TO* __restrict__ out) {
+  using V = typename RowVec<T>::type;
   constexpr int N = RowVec<T>::N;
   const int64_t n = s.rows * k;
   const int32_t kept = (int32_t)min<int64_t>(*kept_ptr, n);
@@ -158,65 +166,142 @@ __global__ __launch_bounds__(kRowThreads) void k_combine(const T* __restrict__ i
     float acc[N];
 #pragma unroll
     for (int e = 0; e < N; ++e) acc[e] = 0.f;
-    for (int j = 0; j < k; ++j) {
-      const int32_t pos = position[t * k + j];
-      if (pos < 0 || pos >= kept) continue;
-      const float w = weights != nullptr ? weight_at<T>(weights, weights_f32, t * k + j) : 1.f;
-      float v[N];
-      load_row<T>(in + pos * stride + c, left, v);
+    for (int j0 = 0; j0 < k; j0 += kSlots) {
+      int32_t pos[kSlots];
+      float w[kSlots];
+      V v[kSlots];
 #pragma unroll
-      for (int e = 0; e < N; ++e) acc[e] = fmaf(w, v[e], acc[e]);
+      for (int u = 0; u < kSlots; ++u) {
+        const int64_t i = t * k + j0 + u;
+        pos[u] = j0 + u < k ? position[i] : -1;
+        w[u] = 1.f;
+        if (weights != nullptr && j0 + u < k) w[u] = weight_at<T>(weights, weights_f32, i);
+      }
+#pragma unroll
+      for (int u = 0; u < kSlots; ++u) {
+        v[u] = V{};
+        if (pos[u] >= 0 && pos[u] < kept) v[u] = load_raw<T, STREAM>(in + pos[u] * stride + c, left);
+      }
+#pragma unroll
+      for (int u = 0; u < kSlots; ++u) {
+        if (pos[u] < 0 || pos[u] >= kept) continue;  // (a dropped slot's weight may be anything)
+#pragma unroll
+        for (int e = 0; e < N; ++e) acc[e] = fmaf(w[u], (float)v[u][e], acc[e]);
+      }
     }
     store_row<TO>(out + t * s.C + c, left, acc);
   });
 }
 
-// One wave per token: grad_in of its slots and the weights' gradients.
-template <typename T, typename TO>
+// The gradients of a token's slots by a group of W lanes (a power of two, or
+// the whole block): grad_out's row is read once for kSlots slots, their rows are
+// in flight together, and each weight's gradient is a sum over the group.
+template <typename T, typename TO, int W, bool STREAM>
 __global__ __launch_bounds__(kRowThreads) void k_combine_backward(
     const TO* __restrict__ grad_out, int64_t grad_stride, const T* __restrict__ in,
     int64_t in_stride, int64_t rows, int k, int C, const void* __restrict__ weights,
     bool weights_f32, const int32_t* __restrict__ position, const int32_t* __restrict__ kept_ptr,
     T* __restrict__ grad_in, void* __restrict__ grad_weights) {
+  using V = typename RowVec<T>::type;
   constexpr int N = RowVec<T>::N;
+  constexpr int kGroups = kRowThreads / W;
+  __shared__ float s_dot[kRowWaves][kSlots];
   const int64_t n = rows * k;
   const int32_t kept = *kept_ptr;
-  const int lane = lane_id();
-  for (int64_t t = (int64_t)blockIdx.x * kRowWaves + threadIdx.x / kWave; t < rows;
-       t += (int64_t)gridDim.x * kRowWaves) {
-    for (int j = 0; j < k; ++j) {
-      const int32_t pos = position[t * k + j];
-      if (pos < 0 || pos >= n) continue;
-      const bool on = pos < kept;
-      const float w = on && grad_in != nullptr ? weight_at<T>(weights, weights_f32, t * k + j) : 0.f;
-      float dot = 0.f;
-      for (int c = lane * N; c < C; c += kWave * N) {
+  const int lane = threadIdx.x % W;
+  const int cv = (C + N - 1) / N;
+  for (int64_t t0 = (int64_t)blockIdx.x * kGroups; t0 < rows; t0 += (int64_t)gridDim.x * kGroups) {
+    // (groups past the end go along for the sums, without slots)
+    const int64_t t = min(t0 + threadIdx.x / W, rows - 1);
+    const bool mine = t0 + threadIdx.x / W < rows;
+    for (int j0 = 0; j0 < k; j0 += kSlots) {
+      int32_t pos[kSlots];
+      float w[kSlots], dot[kSlots];
+#pragma unroll
+      for (int u = 0; u < kSlots; ++u) {
+        const int64_t i = t * k + j0 + u;
+        pos[u] = mine && j0 + u < k ? position[i] : -1;
+        if (pos[u] >= n) pos[u] = -1;
+        w[u] = dot[u] = 0.f;
+        if (pos[u] >= 0 && pos[u] < kept && grad_in != nullptr)
+          w[u] = weight_at<T>(weights, weights_f32, i);
+      }
+      for (int vec = lane; vec < cv; vec += W) {
+        const int c = vector_start<N>(vec, C);
+        const int left = C - c;
+        const int again = vec * N - c;  // elements that the vector before has too
         float g[N];
-        load_row<TO>(grad_out + t * grad_stride + c, C - c, g);
-        if (grad_weights != nullptr && on) {
-          float v[N];
-          load_row<T>(in + pos * in_stride + c, C - c, v);
-  #pragma unroll
-          for (int e = 0; e < N; ++e) dot = fmaf(g[e], v[e], dot);
+        load_row<TO>(grad_out + t * grad_stride + c, left, g);
+        V v[kSlots];
+        if (grad_weights != nullptr) {
+#pragma unroll
+          for (int u = 0; u < kSlots; ++u) {
+            v[u] = V{};
+            if (pos[u] >= 0 && pos[u] < kept) v[u] = load_raw<T, STREAM>(in + pos[u] * in_stride + c, left);
+          }
         }
         if (grad_in != nullptr) {
-  #pragma unroll
-          for (int e = 0; e < N; ++e) g[e] = on ? w * g[e] : 0.f;
-          store_row<T>(grad_in + (int64_t)pos * C + c, C - c, g);
+#pragma unroll
+          for (int u = 0; u < kSlots; ++u) {
+            if (pos[u] < 0) continue;
+            float d[N];
+#pragma unroll
+            for (int e = 0; e < N; ++e) d[e] = pos[u] < kept ? w[u] * g[e] : 0.f;
+            store_row<T, STREAM>(grad_in + (int64_t)pos[u] * C + c, left, d);
+          }
+        }
+        if (grad_weights != nullptr) {
+#pragma unroll
+          for (int u = 0; u < kSlots; ++u) {
+            if (pos[u] < 0 || pos[u] >= kept) continue;
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+              dot[u] = e >= again ? fmaf(g[e], (float)v[u][e], dot[u]) : dot[u];
+          }
         }
       }
-      if (grad_weights != nullptr) {
-  #pragma unroll
-        for (int o = kWave / 2; o > 0; o >>= 1) dot += __shfl_xor(dot, o, kWave);
-        if (lane == 0) {
-          if (weights_f32)
-            static_cast<float*>(grad_weights)[t * k + j] = dot;
-          else
-            static_cast<T*>(grad_weights)[t * k + j] = (T)dot;
+      if (grad_weights == nullptr) continue;
+#pragma unroll
+      for (int u = 0; u < kSlots; ++u)
+#pragma unroll
+        for (int o = min(W, kWave) / 2; o > 0; o >>= 1) dot[u] += __shfl_xor(dot[u], o, kWave);
+      if constexpr (W > kWave) {
+        __syncthreads();  // (the sums of the slots before have been read)
+        if (threadIdx.x % kWave == 0)
+#pragma unroll
+          for (int u = 0; u < kSlots; ++u) s_dot[threadIdx.x / kWave][u] = dot[u];
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < kSlots; ++u) {
+          dot[u] = s_dot[0][u];
+#pragma unroll
+          for (int b = 1; b < kRowWaves; ++b) dot[u] += s_dot[b][u];
         }
+      }
+#pragma unroll
+      for (int u = 0; u < kSlots; ++u) {
+        if (lane != u % W || !mine || j0 + u >= k) continue;
+        const int64_t i = t * k + j0 + u;
+        if (weights_f32) static_cast<float*>(grad_weights)[i] = dot[u];
+        else static_cast<T*>(grad_weights)[i] = (T)dot[u];
       }
     }
   }
+}
+
+// Lanes per token of the combine's gradient: no more than a row has vectors, a
+// whole block for rows that fill it (their k slots then go through DRAM in
+// whole rows: 16,384 tokens of 4 slots, C = 2048 in bfloat16, 130 us by waves
+// and 118 by blocks) and where waves would leave the device empty (fewer than
+// eight to a compute unit).
+template <class F>
+void by_lanes(int64_t rows, int64_t cv, F f) {
+  if (cv >= kRowThreads || (cv > kWave && rows < 2048))
+    f(std::integral_constant<int, kRowThreads>{});
+  else if (cv > 32) f(std::integral_constant<int, kWave>{});
+  else if (cv > 16) f(std::integral_constant<int, 32>{});
+  else if (cv > 8) f(std::integral_constant<int, 16>{});
+  else f(std::integral_constant<int, 8>{});
 }
 
 }  // namespace
@@ -274,9 +359,13 @@ hipError_t launch_combine_forward(int64_t rows, int32_t k, int64_t C, int in_dty
     using T = decltype(ti);
     using TO = decltype(to);
     const RowSplit s = row_split(rows, C, RowVec<T>::N);
-    k_combine<T, TO><<<row_grid(s), kRowThreads, 0, stream>>>(
-        static_cast<const T*>(in), in_stride, s, k, weights, weight_dtype == BEVPOOL_F32, position,
-        kept, static_cast<TO*>(out));
+    auto go = [&](auto hint) {
+      k_combine<T, TO, hint.value><<<row_grid(s), kRowThreads, 0, stream>>>(
+          static_cast<const T*>(in), in_stride, s, k, weights, weight_dtype == BEVPOOL_F32,
+          position, kept, static_cast<TO*>(out));
+    };
+    if (stream_rows(rows * k, C, sizeof(T))) go(std::true_type{});
+    else go(std::false_type{});
   });
   return hipGetLastError();
 }
@@ -287,14 +376,21 @@ hipError_t launch_combine_backward(int64_t rows, int32_t k, int64_t C, int in_dt
                                    const int32_t* position, const int32_t* kept, void* grad_in,
                                    void* grad_weights, hipStream_t stream) {
   if (rows == 0 || (grad_in == nullptr && grad_weights == nullptr)) return hipSuccess;
-  const dim3 grid((unsigned)std::min<int64_t>((rows + kRowWaves - 1) / kRowWaves, kMaxBlocks));
   by_types(in_dtype, out_dtype, [&](auto ti, auto to) {
     using T = decltype(ti);
     using TO = decltype(to);
-    k_combine_backward<T, TO><<<grid, kRowThreads, 0, stream>>>(
-        static_cast<const TO*>(grad_out), grad_stride, static_cast<const T*>(in), in_stride, rows,
-        k, (int)C, weights, weight_dtype == BEVPOOL_F32, position, kept, static_cast<T*>(grad_in),
-        grad_weights);
+    by_lanes(rows, (C + RowVec<T>::N - 1) / RowVec<T>::N, [&](auto w) {
+      constexpr int kGroups = kRowThreads / w.value;
+      const dim3 grid((unsigned)std::min<int64_t>((rows + kGroups - 1) / kGroups, kMaxBlocks));
+      auto go = [&](auto hint) {
+        k_combine_backward<T, TO, w.value, hint.value><<<grid, kRowThreads, 0, stream>>>(
+            static_cast<const TO*>(grad_out), grad_stride, static_cast<const T*>(in), in_stride,
+            rows, k, (int)C, weights, weight_dtype == BEVPOOL_F32, position, kept,
+            static_cast<T*>(grad_in), grad_weights);
+      };
+      if (stream_rows(rows * k, C, sizeof(T))) go(std::true_type{});
+      else go(std::false_type{});
+    });
   });
   return hipGetLastError();
 }

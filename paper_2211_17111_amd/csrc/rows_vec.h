@@ -60,12 +60,16 @@ __device__ __forceinline__ void load_row(const T* p, int left, float (&v)[M]) {
   }
 }
 
-// The vector at p as it is, zeros past `left`, and v += its elements.
-template <typename T>
+// The vector at p as it is, zeros past `left`.  STREAM: the line is not wanted
+// again (a hint to the caches).
+template <typename T, bool STREAM = false>
 __device__ __forceinline__ typename RowVec<T>::type load_raw(const T* p, int left) {
   using V = typename RowVec<T>::type;
   constexpr int N = RowVec<T>::N;
-  if (left >= N) return *reinterpret_cast<const V*>(p);
+  if (left >= N) {
+    if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
+    else return *reinterpret_cast<const V*>(p);
+  }
   V t = {};
 #pragma unroll
   for (int e = 0; e < N; ++e)
@@ -73,7 +77,18 @@ __device__ __forceinline__ typename RowVec<T>::type load_raw(const T* p, int lef
   return t;
 }
 
-template <typename T, int M>
+// Whether rows that a kernel reads (and writes) once are streamed: not where
+// they fit the eight L2s (32 MB), and not below four cache lines a row, where
+// neighbouring rows share lines that other waves want.  Without and with, in
+// microseconds: the combine of 200 MB of bfloat16 rows 57.8 and 73.9 at 80 bytes
+// a row, 48.8 and 47.0 at 512, 48.4 and 46.9 at 4096, of 1.07 GB at 8192 bytes
+// 242 and 214; its gradient 147 and 178, 100 and 87, 98 and 86, and with 20 MB
+// of 512-byte rows 11.3 and 12.0.
+inline bool stream_rows(int64_t rows, int64_t C, size_t element) {
+  return C * (int64_t)element >= 512 && rows * C * (int64_t)element > (int64_t(32) << 20);
+}
+
+template <typename T, bool STREAM = false, int M>
 __device__ __forceinline__ void store_row(T* p, int left, const float (&v)[M]) {
   constexpr int N = RowVec<T>::N < M ? RowVec<T>::N : M;  // (4 of a narrow type, from float32)
   using V = std::conditional_t<N == RowVec<T>::N, typename RowVec<T>::type, typename RowVec<T>::four>;
@@ -84,7 +99,8 @@ __device__ __forceinline__ void store_row(T* p, int left, const float (&v)[M]) {
       V t;
 #pragma unroll
       for (int e = 0; e < N; ++e) t[e] = (T)v[b + e];
-      *reinterpret_cast<V*>(p + b) = t;
+      if constexpr (STREAM) __builtin_nontemporal_store(t, reinterpret_cast<V*>(p + b));
+      else *reinterpret_cast<V*>(p + b) = t;
     }
   } else {
 #pragma unroll
@@ -131,6 +147,17 @@ inline dim3 row_grid(const RowSplit& s) {
               (unsigned)((s.cv + s.cvb - 1) / s.cvb));
 }
 
+// First element of vector c of a row of C elements: a row's last vector ends
+// with the row, over elements of the one before (two lanes then move or sum the
+// same elements alike); a row shorter than a vector has one partial vector.
+// Going through a row's last few elements one by one instead takes every wave
+// that holds one along: rows of 1001 float16 elements, 4 slots a token, were
+// dispatched in 31 us and are in 24.
+template <int N>
+__device__ __forceinline__ int32_t vector_start(int32_t c, int32_t C) {
+  return min(c * N, max(C - N, 0));
+}
+
 // Calls f(row, first element) for every vector of this thread.
 template <int N, class F>
 __device__ __forceinline__ void for_row_vectors(const RowSplit& s, F f) {
@@ -140,7 +167,7 @@ __device__ __forceinline__ void for_row_vectors(const RowSplit& s, F f) {
     for (uint32_t i = threadIdx.x; i < (uint32_t)(rows * s.cvb); i += kRowThreads) {
       const uint32_t r = s.by.div(i);
       const int32_t c = c0 + (int32_t)(i - r * (uint32_t)s.cvb);
-      if (c < s.cv) f(row0 + r, c * N);
+      if (c < s.cv) f(row0 + r, vector_start<N>(c, s.C));
     }
   }
 }

@@ -251,6 +251,45 @@ def test_dispatch_and_combine(T, k, E, C, dtype, kind):
             assert none is None and torch.equal(only, grad_w)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,k,C", [(5003, 4, 1027), (2100, 9, 1024), (40000, 3, 300)])
+def test_many_rows(T, k, C, dtype):
+    """Sizes past the caches, where rows are streamed: against float64 on the device."""
+    say(f"many rows T={T} k={k} C={C} {dtype}")
+    E = 40
+    ids = torch.from_numpy(_ids(T, k, E, 8)).to(DEV)
+    x, y = _normal(T, C, dtype=dtype), _normal(T * k, C, dtype=dtype, seed=1)
+    assert y.numel() * y.element_size() > 32 << 20
+    w, g = _normal(T, k, seed=2), _normal(T, C, dtype=dtype, seed=3)
+    r, plan = rows.dispatch_forward(x, ids, E)
+    kept = int(plan.offsets[-1])
+    assert torch.equal(r[:kept], x[plan.order[:kept].long() // k]) and not r[kept:].any()
+    pos = plan.position.long().view(T, k)
+    on = (pos < kept)[..., None]
+    mine = torch.where(on, y[pos], 0).double()
+
+    def check(got, want, bound, label):
+        half = want.abs() * torch.finfo(got.dtype).eps / 2 + torch.finfo(got.dtype).smallest_normal
+        assert ((got.double() - want).abs() <= bound + half * (1 + 2 * U)).all(), label
+
+    terms = w.double()[..., None] * mine
+    check(rows.combine_forward(y, w, plan), terms.sum(1), (k + 2) * U * terms.abs().sum(1), "combine")
+    check(rows.dispatch_backward(y, plan, k), mine.sum(1), (k + 2) * U * mine.abs().sum(1), "dispatch gradient")
+    grad_rows, grad_w = rows.combine_backward(g, y, w, plan)
+    want = torch.where(on, w.double()[..., None] * g.double()[:, None], 0.0)
+    check(grad_rows[pos.view(-1)].view(T, k, C), want, U * want.abs(), "gradient of the rows")
+    terms = mine * g.double()[:, None]
+    check(grad_w, terms.sum(2), (C + 2) * U * terms.abs().sum(2), "gradient of the weights")
+    V = 1000
+    eids = torch.randint(-1, V, (T * k,), device=DEV)
+    want, mag = torch.zeros(V + 1, C, dtype=torch.float64, device=DEV), torch.zeros(V + 1, C, dtype=torch.float64, device=DEV)
+    row = torch.where(eids >= 0, eids, V)
+    want.index_add_(0, row, y.double())
+    mag.index_add_(0, row, y.double().abs())
+    n = torch.bincount(row, minlength=V + 1)[:V, None]
+    check(rows.embed_backward(y, eids, V), want[:V], (n + 2) * U * mag[:V], "embedding gradient")
+
+
 def test_rows_behind_the_kept_ones_are_not_used():
     """Infinities and NaN in rows of dropped slots reach nothing."""
     T, k, E, C = 20, 3, 4, 40

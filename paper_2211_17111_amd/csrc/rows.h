@@ -24,7 +24,8 @@ struct SortLayout {
 };
 SortLayout sort_layout(int64_t n, int64_t n_keys);
 
-// position or sorted_keys (n_keys for a dropped slot) may be NULL.
+// position and sorted_keys (n_keys for a dropped slot) may be NULL, and offsets
+// with several passes.
 hipError_t launch_sort_keys(int64_t n, int64_t n_keys, int key_type, const void* keys,
                             int32_t* order, int32_t* position, int32_t* offsets,
                             int32_t* sorted_keys, void* workspace, hipStream_t stream);

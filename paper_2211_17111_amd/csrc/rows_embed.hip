@@ -5,6 +5,7 @@
 
 #include "device_utils.h"
 #include "rows.h"
+#include "rows_sort.h"
 #include "rows_vec.h"
 
 namespace bevpool {
@@ -52,23 +53,31 @@ __global__ __launch_bounds__(kRowThreads) void k_embed(const T* __restrict__ tab
 struct Ranges {
   const int32_t* order;
   const int32_t* keys;     // of the sorted slots
-  const int32_t* offsets;  // [n_keys + 1]
+  int32_t* offsets;        // [n_keys + 1]
   float* partials;         // [2 * ranges][C]
+  int64_t n;               // slots
   int64_t ranges;
   int32_t RG;
   int32_t n_keys;
   int32_t C;
 };
 
-constexpr int kInFlight = 8;  // rows a lane group has in flight
+constexpr int kInFlight = 8;   // rows a lane group has in flight
+constexpr int kJoinFlight = 4;  // and partials
 
 template <typename T, typename TO, bool STREAM>
 __global__ __launch_bounds__(kRowThreads) void k_embed_ranges(const T* __restrict__ grad_out,
-                                                              int64_t stride, Ranges a, int32_t W,
+                                                              int64_t stride, Ranges a,
+                                                              unsigned range_blocks, int32_t W,
                                                               int32_t tiles, float scale,
                                                               TO* __restrict__ grad_table) {
   using V = typename RowVec<T>::type;
   constexpr int N = RowVec<T>::N;
+  if (blockIdx.x >= range_blocks) {  // (an id to a thread, where the sort has not left the offsets)
+    const int64_t v = (int64_t)(blockIdx.x - range_blocks) * kRowThreads + threadIdx.x;
+    if (v <= a.n_keys) a.offsets[v] = (int32_t)keys_below(a.keys, a.n, v);
+    return;
+  }
   // group of W lanes: one range, vectors [tile W, tile W + W) of its rows
   const int group = threadIdx.x / W;
   const int G = kRowThreads / W;
@@ -80,23 +89,24 @@ __global__ __launch_bounds__(kRowThreads) void k_embed_ranges(const T* __restric
   if (vec * N >= a.C) return;
   const int c = vector_start<N>(vec, a.C);
   const int left = a.C - c;
-  const int32_t kept = a.offsets[a.n_keys];
   const int64_t p0 = r * a.RG;
-  const int32_t m = (int32_t)min<int64_t>(a.RG, kept - p0);  // (<= 0 behind the kept slots)
-  if (m <= 0) return;
+  const int32_t m = (int32_t)min<int64_t>(a.RG, a.n - p0);
   const int32_t before = p0 > 0 ? a.keys[p0 - 1] : -1;
-  const int32_t after = p0 + m < kept ? a.keys[p0 + m] : -1;
+  const int32_t after = p0 + m < a.n ? a.keys[p0 + m] : -1;
   const int32_t* order = a.order + p0;
   const int32_t* keys = a.keys + p0;
   float acc[N];
 #pragma unroll
   for (int e = 0; e < N; ++e) acc[e] = 0.f;
   int32_t cur = keys[0];
+  if (cur >= a.n_keys) return;  // (dropped slots, like all behind them)
   auto flush = [&]() {
-    if (cur == before || cur == after) {
+    if (cur >= a.n_keys) {
+      // (dropped slots at the end of the kept ones)
+    } else if (cur == before || cur == after) {
       const int64_t slot = 2 * r + (cur == before ? 0 : 1);
       store_row<float>(a.partials + slot * a.C + c, left, acc);
-    } else if (cur >= 0 && cur < a.n_keys) {
+    } else if (cur >= 0) {
 #pragma unroll
       for (int e = 0; e < N; ++e) acc[e] *= scale;
       store_row<TO>(grad_table + (int64_t)cur * a.C + c, left, acc);
@@ -127,11 +137,36 @@ __global__ __launch_bounds__(kRowThreads) void k_embed_ranges(const T* __restric
   flush();
 }
 
-// Blocks [0, fill): rows of ids that do not occur.  The others: (range, 64
-// vectors of 4 elements) each.
+// Adds the n partials from j0 on, `step` apart, of an id that starts in range r.
+template <int N>
+__device__ __forceinline__ void add_partials(const Ranges& a, int64_t r, int64_t j0, int64_t step,
+                                             int64_t n, int c, float (&acc)[N]) {
+  // (the second partial of the range where it starts, the first of the others)
+  auto at = [&](int64_t j) { return a.partials + (2 * (r + j) + (j == 0 ? 1 : 0)) * a.C + c; };
+  int64_t j = j0;
+  for (; j + (kJoinFlight - 1) * step < n; j += kJoinFlight * step) {
+    float g[kJoinFlight][N];
+#pragma unroll
+    for (int u = 0; u < kJoinFlight; ++u) load_row<float>(at(j + u * step), a.C - c, g[u]);
+#pragma unroll
+    for (int u = 0; u < kJoinFlight; ++u)
+#pragma unroll
+      for (int e = 0; e < N; ++e) acc[e] += g[u][e];
+  }
+  for (; j < n; j += step) {
+    float g[N];
+    load_row<float>(at(j), a.C - c, g);
+#pragma unroll
+    for (int e = 0; e < N; ++e) acc[e] += g[e];
+  }
+}
+
+// Blocks [0, fill): rows of ids that do not occur.  The others: ranges of one
+// tile of W vectors of 4 elements, one to each of the block's G lane groups;
+// a group joins an id of a few partials, the whole block one of more.
 template <typename TO>
 __global__ __launch_bounds__(kRowThreads) void k_embed_rest(RowSplit s, Ranges a, int64_t fill,
-                                                            int32_t tiles, float scale,
+                                                            int32_t W, int32_t tiles, float scale,
                                                             TO* __restrict__ grad_table) {
   if (blockIdx.x < fill) {
     constexpr int N = RowVec<TO>::N;
@@ -151,58 +186,56 @@ __global__ __launch_bounds__(kRowThreads) void k_embed_rest(RowSplit s, Ranges a
     }
     return;
   }
-  const int64_t item = blockIdx.x - fill;
-  const int64_t r = item / tiles;
-  const int32_t kept = a.offsets[a.n_keys];
-  const int64_t p1 = (r + 1) * a.RG;  // first slot of the next range
-  if (p1 >= kept) return;             // (the same for the whole block, as what follows)
-  const int32_t v = a.keys[p1];
-  if (a.keys[p1 - 1] != v || v < 0 || v >= a.n_keys) return;
-  const int32_t begin = a.offsets[v], end = a.offsets[v + 1];
-  if (begin < p1 - a.RG || begin >= p1 || end <= p1) return;  // (it starts in an earlier range)
-  const int64_t last = (end - 1) / a.RG;
   constexpr int N = 4;
+  constexpr int kMaxGroups = kRowThreads;
   __shared__ float s_sum[kRowThreads][N + 1];
-  const int cv = (a.C + N - 1) / N;
-  const int first_vec = (int)(item - r * tiles) * kWave;
-  const int W = min(kWave, cv - first_vec);
+  __shared__ int32_t s_many[kMaxGroups];  // partials that the block has to join for each group, or 0
   const int G = kRowThreads / W;
   const int group = threadIdx.x / W;
-  const int c = vector_start<N>(first_vec + threadIdx.x - group * W, a.C);
-  float acc[N] = {};
-  if (group < G) {
-    // the id's partial of range r + j: the second in the range where it starts
-    auto at = [&](int64_t j) {
-      return a.partials + (2 * (r + j) + (j == 0 ? 1 : 0)) * a.C + c;
-    };
-    const int64_t n = last - r + 1;
-    int64_t j = group;
-    for (; j + (kInFlight - 1) * G < n; j += kInFlight * G) {
-      float g[kInFlight][N];
-#pragma unroll
-      for (int u = 0; u < kInFlight; ++u) load_row<float>(at(j + u * G), a.C - c, g[u]);
-#pragma unroll
-      for (int u = 0; u < kInFlight; ++u)
-#pragma unroll
-        for (int e = 0; e < N; ++e) acc[e] += g[u][e];
-    }
-    for (; j < n; j += G) {
-      float g[N];
-      load_row<float>(at(j), a.C - c, g);
-#pragma unroll
-      for (int e = 0; e < N; ++e) acc[e] += g[e];
-    }
-  }
-#pragma unroll
-  for (int e = 0; e < N; ++e) s_sum[threadIdx.x][e] = acc[e];
-  __syncthreads();
-  if (group == 0) {
-    for (int g = 1; g < G; ++g)
-#pragma unroll
-      for (int e = 0; e < N; ++e) acc[e] += s_sum[g * W + threadIdx.x][e];
+  const int64_t item = blockIdx.x - fill;
+  const int64_t r0 = item / tiles * G;
+  const int vec = (int)(item % tiles) * W + threadIdx.x - group * W;
+  const bool on = group < G && vec * N < a.C;
+  const int c = vector_start<N>(vec, a.C);
+  // the id that starts in range r and goes on: its number of partials, or 0
+  auto partials_from = [&](int64_t r, int32_t& v) -> int64_t {
+    const int64_t p1 = (r + 1) * a.RG;  // first slot of the next range
+    if (r >= a.ranges || p1 >= a.n) return 0;
+    v = a.keys[p1];
+    if (a.keys[p1 - 1] != v || v < 0 || v >= a.n_keys) return 0;
+    const int32_t begin = a.offsets[v], end = a.offsets[v + 1];
+    if (begin < p1 - a.RG || begin >= p1 || end <= p1) return 0;  // (it starts in an earlier range)
+    return (end - 1) / a.RG - r + 1;
+  };
+  auto finish = [&](int32_t v, float (&acc)[N]) {
 #pragma unroll
     for (int e = 0; e < N; ++e) acc[e] *= scale;
     store_row<TO>(grad_table + (int64_t)v * a.C + c, a.C - c, acc);
+  };
+  int32_t v = 0;
+  const int64_t n = group < G ? partials_from(r0 + group, v) : 0;
+  if (on && n > 0 && n <= kJoinFlight) {
+    float acc[N] = {};
+    add_partials<N>(a, r0 + group, 0, 1, n, c, acc);
+    finish(v, acc);
+  }
+  if (group < G && threadIdx.x == group * W) s_many[group] = n > kJoinFlight ? (int32_t)n : 0;
+  __syncthreads();
+  for (int q = 0; q < G; ++q) {
+    const int32_t many = s_many[q];
+    if (many == 0) continue;  // (uniform over the block)
+    float acc[N] = {};
+    if (on) add_partials<N>(a, r0 + q, group, G, many, c, acc);
+#pragma unroll
+    for (int e = 0; e < N; ++e) s_sum[threadIdx.x][e] = acc[e];
+    __syncthreads();
+    if (group == 0 && on) {
+      for (int g = 1; g < G; ++g)
+#pragma unroll
+        for (int e = 0; e < N; ++e) acc[e] += s_sum[g * W + threadIdx.x][e];
+      finish(a.keys[(r0 + q + 1) * a.RG], acc);
+    }
+    __syncthreads();  // (the sums have been read)
   }
 }
 
@@ -274,24 +307,33 @@ hipError_t launch_embed_backward(int64_t n, int64_t table_rows, int64_t C, int i
   int32_t* order = reinterpret_cast<int32_t*>(ws + L.order);
   int32_t* keys = reinterpret_cast<int32_t*>(ws + L.keys);
   int32_t* offsets = reinterpret_cast<int32_t*>(ws + L.offsets);
-  const hipError_t e = launch_sort_keys(n, table_rows, key_type, ids, order, nullptr, offsets, keys,
-                                        ws + L.sort, stream);
+  const bool search = n > 0 && sort_layout(n, table_rows).passes > 1;
+  const hipError_t e = launch_sort_keys(n, table_rows, key_type, ids, order, nullptr,
+                                        search ? nullptr : offsets, keys, ws + L.sort, stream);
   if (e != hipSuccess) return e;
-  const Ranges a{order, keys, offsets, reinterpret_cast<float*>(ws + L.partials),
+  const Ranges a{order, keys, offsets, reinterpret_cast<float*>(ws + L.partials), n,
                  L.ranges, L.RG, (int32_t)table_rows, (int32_t)C};
+  // lanes of a group and column tiles, for vectors of `per` elements
+  auto lanes = [&](int64_t per, int64_t* tiles) {
+    const int64_t cv = (C + per - 1) / per;
+    *tiles = (cv + kWave - 1) / kWave;
+    return (int32_t)((cv + *tiles - 1) / *tiles);
+  };
   by_any_types(in_dtype, out_dtype, [&](auto ti, auto to) {
     using T = decltype(ti);
     using TO = decltype(to);
     TO* out = static_cast<TO*>(grad_table);
+    int64_t tiles;
     if (n > 0) {
-      const int64_t cv = (C + RowVec<T>::N - 1) / RowVec<T>::N;
-      const int64_t tiles = (cv + kWave - 1) / kWave;
-      const int32_t W = (int32_t)((cv + tiles - 1) / tiles);
+      const int32_t W = lanes(RowVec<T>::N, &tiles);
       const int64_t G = kRowThreads / W;
-      auto go = [&](auto stream_hint) {
-        k_embed_ranges<T, TO, stream_hint.value>
-            <<<(unsigned)((L.ranges * tiles + G - 1) / G), kRowThreads, 0, stream>>>(
-                static_cast<const T*>(grad_out), grad_stride, a, W, (int32_t)tiles, scale, out);
+      const int64_t blocks = (L.ranges * tiles + G - 1) / G;
+      const int64_t searches = search ? table_rows / kRowThreads + 1 : 0;
+      auto go = [&](auto hint) {
+        k_embed_ranges<T, TO, hint.value>
+            <<<(unsigned)(blocks + searches), kRowThreads, 0, stream>>>(
+                static_cast<const T*>(grad_out), grad_stride, a, (unsigned)blocks, W,
+                (int32_t)tiles, scale, out);
       };
       if (stream_rows(n, C, sizeof(T))) go(std::true_type{});
       else go(std::false_type{});
@@ -299,10 +341,11 @@ hipError_t launch_embed_backward(int64_t n, int64_t table_rows, int64_t C, int i
     const RowSplit s = row_split(table_rows, C, RowVec<TO>::N);
     const int64_t parts = (s.cv + s.cvb - 1) / s.cvb;
     const int64_t fill = std::min((s.rows + s.R - 1) / s.R, std::max<int64_t>(1, kMaxBlocks / parts)) * parts;
-    const int64_t tiles = ((C + 3) / 4 + kWave - 1) / kWave;
-    const int64_t joins = L.ranges > 1 ? (L.ranges - 1) * tiles : 0;
+    const int32_t W = lanes(4, &tiles);
+    const int64_t G = kRowThreads / W;
+    const int64_t joins = L.ranges > 1 ? (L.ranges + G - 1) / G * tiles : 0;
     k_embed_rest<TO><<<(unsigned)(fill + joins), kRowThreads, 0, stream>>>(
-        s, a, fill, (int32_t)tiles, scale, out);
+        s, a, fill, W, (int32_t)tiles, scale, out);
   });
   return hipGetLastError();
 }

@@ -13,6 +13,16 @@ constexpr int kTileWaves = kTileThreads / kWave;
 constexpr int kTileRounds = kSortTile / kTileThreads;  // rounds of 64 slots of a wave
 constexpr int kDigitsPerThread = kMaxDigits / kTileThreads;
 
+// Number of the n sorted keys below v.
+__device__ __forceinline__ int64_t keys_below(const int32_t* keys, int64_t n, int64_t v) {
+  int64_t lo = 0, hi = n;
+  while (lo < hi) {
+    const int64_t mid = (lo + hi) >> 1;
+    if (keys[mid] < v) lo = mid + 1; else hi = mid;
+  }
+  return lo;
+}
+
 // The tile's slot that this thread holds in round r: a wave's are consecutive.
 __device__ __forceinline__ int tile_index(int r) {
   return (int)(threadIdx.x / kWave) * kTileRounds * kWave + r * kWave + (int)(threadIdx.x % kWave);

@@ -272,13 +272,7 @@ __global__ __launch_bounds__(256) void k_keys_offsets(const int32_t* __restrict_
                                                       int32_t n_keys,
                                                       int32_t* __restrict__ offsets) {
   const int64_t v = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (v > n_keys) return;
-  int64_t lo = 0, hi = n;
-  while (lo < hi) {
-    const int64_t mid = (lo + hi) >> 1;
-    if (keys[mid] < v) lo = mid + 1; else hi = mid;
-  }
-  offsets[v] = (int32_t)lo;
+  if (v <= n_keys) offsets[v] = (int32_t)keys_below(keys, n, v);
 }
 
 }  // namespace
@@ -333,7 +327,8 @@ hipError_t launch_sort_keys(int64_t n, int64_t n_keys, int key_type, const void*
     };
     if (key_type == BEVPOOL_KEY_I64) go(static_cast<const int64_t*>(keys));
     else go(static_cast<const int32_t*>(keys));
-    if (L.passes > 1) k_keys_offsets<<<ogrid, 256, 0, stream>>>(sorted, n, nk, offsets);
+    if (L.passes > 1 && offsets != nullptr)
+      k_keys_offsets<<<ogrid, 256, 0, stream>>>(sorted, n, nk, offsets);
     return hipGetLastError();
   }
   int32_t *tile_counts = W(L.tile_counts), *group_counts = W(L.group_counts);
@@ -369,7 +364,8 @@ hipError_t launch_sort_keys(int64_t n, int64_t n_keys, int key_type, const void*
     in_keys = out_keys;
     in_slots = out_slots;
   }
-  if (L.passes > 1) k_keys_offsets<<<ogrid, 256, 0, stream>>>(in_keys, n, nk, offsets);
+  if (L.passes > 1 && offsets != nullptr)
+    k_keys_offsets<<<ogrid, 256, 0, stream>>>(in_keys, n, nk, offsets);
   return hipGetLastError();
 }
 

@@ -39,6 +39,7 @@ BEVPOOL_KEY_I32, BEVPOOL_KEY_I64 = 0, 1
 
 _DTYPE_CODE = {torch.float32: _bp.BEVPOOL_F32, torch.float16: _bp.BEVPOOL_F16, torch.bfloat16: BEVPOOL_BF16}
 _KEY_CODE = {torch.int32: BEVPOOL_KEY_I32, torch.int64: BEVPOOL_KEY_I64}
+_I32, _F32 = (torch.int32,), (torch.float32,)
 
 _vp, _i32, _i64, _int, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_int, ctypes.c_size_t
 _ARGTYPES = {
@@ -88,6 +89,9 @@ def _size(name: str, *args) -> int:
     return n.value
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
 def _stream(dev: torch.device) -> int:
     """Handle of dev's current stream (torch's raw query costs a tenth of a stream object)."""
     return _bp._raw_stream(dev.index) if _bp._raw_stream else torch.cuda.current_stream(dev).cuda_stream
@@ -106,7 +110,7 @@ def _matrix(t, name: str, dev: torch.device, dtype=None, shape=None) -> int:
     distance between its rows."""
     if not isinstance(t, torch.Tensor) or t.device != dev:
         raise ValueError(f"{name} must be a tensor on {dev}")
-    if t.dim() != 2 or (shape is not None and tuple(t.shape) != shape):
+    if t.dim() != 2 or (shape is not None and t.shape != shape):
         raise ValueError(f"{name} must be {shape or 'a matrix'}, got {tuple(t.shape)}")
     if t.dtype not in _DTYPE_CODE or (dtype is not None and t.dtype != dtype):
         raise ValueError(f"{name} must be {dtype or 'float32, float16 or bfloat16'}, got {t.dtype}")
@@ -120,7 +124,7 @@ def _dense(t, name: str, dev: torch.device, dtypes, shape=None) -> None:
         raise ValueError(f"{name} must be a tensor on {dev}")
     if t.dtype not in dtypes:
         raise ValueError(f"{name} must be one of {[str(d) for d in dtypes]}, got {t.dtype}")
-    if shape is not None and tuple(t.shape) != shape:
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name} must be {shape}, got {tuple(t.shape)}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
@@ -130,7 +134,7 @@ def _elsewhere(dev: torch.device, stream, *inputs):
     """A context in which dev and `stream` are current, or None where they
     already are: allocations and launches then belong to that stream."""
     if stream is None:
-        return None if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
+        return None if dev.index == _current_device() else torch.cuda.device(dev)
     if not isinstance(stream, torch.cuda.Stream):
         stream = torch.cuda.ExternalStream(int(stream), device=dev)
     if stream.device != dev:
@@ -153,12 +157,13 @@ class KeyOrder:
 
     def _check(self, dev: torch.device, n: int) -> int:
         """Address of the number of kept slots."""
-        _dense(self.position, "position", dev, (torch.int32,))
-        _dense(self.offsets, "offsets", dev, (torch.int32,))
-        if self.position.numel() != n or self.offsets.numel() != self.n_keys + 1:
-            raise ValueError(f"the order has {self.position.numel()} slots and {self.offsets.numel()} offsets; "
-                             f"{n} slots and {self.n_keys + 1} offsets are needed")
-        return self.offsets.data_ptr() + 4 * self.n_keys
+        position, offsets, n_keys = self.position, self.offsets, self.n_keys
+        _dense(position, "position", dev, _I32)
+        _dense(offsets, "offsets", dev, _I32)
+        if position.numel() != n or offsets.numel() != n_keys + 1:
+            raise ValueError(f"the order has {position.numel()} slots and {offsets.numel()} offsets; "
+                             f"{n} slots and {n_keys + 1} offsets are needed")
+        return offsets.data_ptr() + 4 * n_keys
 
 
 def _key_order(n: int, n_keys: int, dev: torch.device):
@@ -215,9 +220,9 @@ def route_backward(grad_weights: torch.Tensor, logits: torch.Tensor, weights: to
     stride = _matrix(logits, "logits", dev)
     T, E = logits.shape
     k = ids.shape[-1]
-    _dense(grad_weights, "grad_weights", dev, (torch.float32,), (T, k))
-    _dense(weights, "weights", dev, (torch.float32,), (T, k))
-    _dense(ids, "ids", dev, (torch.int32,), (T, k))
+    _dense(grad_weights, "grad_weights", dev, _F32, (T, k))
+    _dense(weights, "weights", dev, _F32, (T, k))
+    _dense(ids, "ids", dev, _I32, (T, k))
     ctx = _elsewhere(dev, stream, grad_weights, logits, weights, ids)
     if ctx is not None:
         with ctx:

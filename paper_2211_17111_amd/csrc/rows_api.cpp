@@ -99,6 +99,18 @@ int check_weight_dtype(int weight_dtype, int in_dtype) {
   return BEVPOOL_OK;
 }
 
+// A launch holds fewer than 2^24 blocks of 256 threads: the kernels of the
+// table's gradient have at most a quarter block per range of slots and 256
+// elements of a row, beside those over the table.  (Only the expanded gradient
+// of more elements than fit the device's memory comes near.)
+int check_embed_grid(int64_t n, int64_t table_rows, int64_t C) {
+  const int64_t ranges = bevpool::embed_layout(n, table_rows, C).ranges;
+  if (ranges * ((C + 255) / 256) > (int64_t(1) << 24))
+    return fail(BEVPOOL_EOVERFLOW, "n * C = %lld * %lld exceeds the gradient's launch", (long long)n,
+                (long long)C);
+  return BEVPOOL_OK;
+}
+
 #define CHECK(call)                        \
   do {                                     \
     const int st_ = (call);                \
@@ -295,6 +307,7 @@ int bevpool_embed_backward_workspace_size(int64_t n, int64_t table_rows, int64_t
                                           size_t* bytes) {
   CHECK(check_keys(n, table_rows));
   CHECK(check_columns(C));
+  CHECK(check_embed_grid(n, table_rows, C));
   REQUIRE_PTR(bytes);
   *bytes = bevpool::embed_layout(n, table_rows, C).total;
   return ok();
@@ -306,6 +319,7 @@ int bevpool_embed_backward(int64_t n, int64_t table_rows, int64_t C, int in_dtyp
                            size_t workspace_bytes, void* stream) {
   CHECK(check_keys(n, table_rows));
   CHECK(check_columns(C));
+  CHECK(check_embed_grid(n, table_rows, C));
   if (in_dtype == BEVPOOL_F32)
     CHECK(check_dtype(out_dtype, "out_dtype"));
   else

@@ -173,7 +173,8 @@ __global__ __launch_bounds__(kRowThreads) void k_embed_rest(RowSplit s, Ranges a
     const float zero[N] = {};
     const int32_t parts = (s.cv + s.cvb - 1) / s.cvb;
     const int32_t c0 = (int32_t)(blockIdx.x % parts) * s.cvb;
-    for (int64_t row0 = blockIdx.x / parts * s.R; row0 < s.rows; row0 += fill / parts * s.R) {
+    for (int64_t row0 = (int64_t)(blockIdx.x / parts) * s.R; row0 < s.rows;
+         row0 += fill / parts * s.R) {
       const int32_t items = (int32_t)min<int64_t>(s.R, s.rows - row0) * s.cvb;
       for (uint32_t i = threadIdx.x; i < (uint32_t)items; i += kRowThreads) {
         const uint32_t q = s.by.div(i);

@@ -452,8 +452,8 @@ class DispatchFunction(torch.autograd.Function):
 class CombineFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, rows, weights, plan, out_dtype):
-        ctx.plan = plan
-        ctx.save_for_backward(rows, weights)
+        ctx.n_keys = plan.n_keys
+        ctx.save_for_backward(rows, weights, plan.position, plan.offsets)
         ctx.set_materialize_grads(False)
         return combine_forward(rows, weights, plan, out_dtype)
 
@@ -462,8 +462,9 @@ class CombineFunction(torch.autograd.Function):
     def backward(ctx, grad_out):
         if grad_out is None:
             return None, None, None, None
-        rows, weights = ctx.saved_tensors
-        return *combine_backward(_rows_apart(grad_out), rows, weights, ctx.plan, *ctx.needs_input_grad[:2]), None, None
+        rows, weights, position, offsets = ctx.saved_tensors
+        plan = KeyOrder(position, position, offsets, ctx.n_keys)
+        return *combine_backward(_rows_apart(grad_out), rows, weights, plan, *ctx.needs_input_grad[:2]), None, None
 
 
 class EmbedFunction(torch.autograd.Function):

@@ -101,6 +101,22 @@ def test_sort_keys_extreme_values():
             _same_plan(plan, ref.sort_keys_ref(keys, n_keys), f"{n_keys} {dtype}")
 
 
+@pytest.mark.parametrize("n", [262144, 262145, 1500007])
+@pytest.mark.parametrize("n_keys", [3, 900, 70000, 1 << 21])
+def test_sort_many_keys(n, n_keys):
+    """More groups of tiles than a block adds up itself, against torch's stable sort."""
+    say(f"sort_keys n={n} n_keys={n_keys}")
+    g = torch.Generator(device=DEV).manual_seed(n + n_keys)
+    keys = torch.randint(-n_keys // 9 - 1, n_keys + n_keys // 9 + 1, (n,), generator=g, device=DEV)
+    keys[n // 3:n // 2] = n_keys // 2  # a frequent one
+    plan = rows.sort_keys(keys, n_keys)
+    k = torch.where((keys >= 0) & (keys < n_keys), keys, n_keys)
+    ordered, order = torch.sort(k, stable=True)
+    assert torch.equal(plan.order.long(), order)
+    assert torch.equal(plan.position[order].long(), torch.arange(n, device=DEV))
+    assert torch.equal(plan.offsets.long(), torch.searchsorted(ordered, torch.arange(n_keys + 1, device=DEV)))
+
+
 # -------------------------------------------------------------------- router
 
 def _logits(T, E, dtype, seed, kind="plain"):
@@ -394,6 +410,43 @@ def test_embed_places_past_32_bits():
     assert torch.equal(grad[V - 1], (out[0].float() + out[3].float()).to(BF16))
     assert torch.equal(grad[V // 2], out[2]) and torch.equal(grad[0], out[1])
     assert not grad[1:V // 2].any() and not grad[V // 2 + 1:V - 1].any()
+
+
+@pytest.mark.parametrize("n,V,C,kind", [(400000, 5, 12, "zipf"), (400000, 300000, 20, "even"), (300000, 2000, 40, "one")])
+def test_embed_gradient_of_many_slots(n, V, C, kind):
+    """Long ranges, and ids of hundreds of ranges, against float64 on the device."""
+    say(f"embedding gradient n={n} V={V} C={C} {kind}")
+    ids = torch.from_numpy(_keys(n, V, 3, kind)).to(DEV)
+    g = _normal(n, C, seed=1)
+    row = torch.where((ids >= 0) & (ids < V), ids, V)
+    want, mag = (torch.zeros(V + 1, C, dtype=torch.float64, device=DEV) for _ in range(2))
+    want.index_add_(0, row, g.double())
+    mag.index_add_(0, row, g.double().abs())
+    count = torch.bincount(row, minlength=V + 1)[:V, None]
+    got = rows.embed_backward(g, ids, V)
+    assert ((got.double() - want[:V]).abs() <= (count + 2) * U * mag[:V] + 1e-30).all()
+    assert not got[count[:, 0] == 0].any()
+
+
+def test_dispatch_and_combine_past_32_bits():
+    """Slots' rows that lie more than 2^32 elements in."""
+    T, k, C, E = (1 << 18) + 5, 4, 4104, 8  # 4.3e9 elements of rows
+    x = torch.randn((T, C), dtype=BF16, device=DEV)
+    ids = torch.randint(0, E, (T, k), device=DEV)
+    r, plan = rows.dispatch_forward(x, ids, E)
+    for q in (0, T * k // 2, T * k - 2, T * k - 1):
+        assert torch.equal(r[q], x[int(plan.order[q]) // k]), q
+    w = torch.full((T, k), 0.25, device=DEV)
+    assert torch.equal(rows.combine_forward(r, w, plan), x)  # (four quarters: exact)
+    grad_rows, grad_w = rows.combine_backward(x, r, w, plan)
+    for q in (0, T * k // 2, T * k - 1):
+        assert torch.equal(grad_rows[q], (0.25 * x[int(plan.order[q]) // k].float()).to(BF16)), q
+    t = torch.tensor([0, T // 2, T - 1], device=DEV)
+    want = x[t].double().square().sum(1, keepdim=True)
+    assert ((grad_w[t].double() - want).abs() <= (C + 2) * U * want).all()
+    del grad_rows, grad_w
+    back = rows.dispatch_backward(r, plan, k)
+    assert torch.equal(back, (4 * x.float()).to(BF16))
 
 
 # ------------------------------------------------------------ used together

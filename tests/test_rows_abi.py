@@ -183,6 +183,9 @@ def test_embed_refusals(lib):
     n = ctypes.c_size_t()
     assert lib.bevpool_embed_backward_workspace_size(5, 5, 0, ctypes.byref(n)) == EINVAL
     assert lib.bevpool_embed_backward_workspace_size(5, 5, 8, None) == EINVAL
+    # more blocks than a launch holds (an expanded gradient could ask for it)
+    assert lib.bevpool_embed_backward_workspace_size((1 << 31) - 1, 5, 1 << 20, ctypes.byref(n)) == EOVERFLOW
+    assert bwd(n=(1 << 31) - 1, C=1 << 20) == EOVERFLOW
     assert lib.bevpool_embed_backward_workspace_size(0, 5, 8, ctypes.byref(n)) == OK and n.value > 0
 
 

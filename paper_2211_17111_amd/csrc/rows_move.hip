@@ -223,8 +223,7 @@ __global__ __launch_bounds__(kRowThreads) void k_combine_backward(
         pos[u] = mine && j0 + u < k ? position[i] : -1;
         if (pos[u] >= n) pos[u] = -1;
         w[u] = dot[u] = 0.f;
-        if (pos[u] >= 0 && pos[u] < kept && grad_in != nullptr)
-          w[u] = weight_at<T>(weights, weights_f32, i);
+        if (grad_in != nullptr && j0 + u < k) w[u] = weight_at<T>(weights, weights_f32, i);
       }
       for (int vec = lane; vec < cv; vec += W) {
         const int c = vector_start<N>(vec, C);

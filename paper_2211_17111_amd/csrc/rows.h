@@ -14,13 +14,15 @@ namespace bevpool {
 // keys 0 .. n_keys (n_keys = dropped).
 constexpr int kSortBits = 10;
 constexpr int kSortTile = 1024;
-constexpr int kSmallSort = 4096;  // most slots that one workgroup sorts
+// Most slots that one workgroup sorts, in one pass and in several.
+constexpr int kSmallSort = 4096, kSmallSortPasses = 8192;
 struct SortLayout {
   size_t tile_counts, group_counts, totals;  // int32[digits] per tile, per group, in all
   size_t keys[2], vals[2];                   // int32[n] each, with several passes
   size_t total;                              // bytes
   int64_t tiles, groups;
   int bits, passes, digit_bits;
+  bool small;  // one workgroup
 };
 SortLayout sort_layout(int64_t n, int64_t n_keys);
 

@@ -28,15 +28,20 @@ __device__ __forceinline__ int tile_index(int r) {
   return (int)(threadIdx.x / kWave) * kTileRounds * kWave + r * kWave + (int)(threadIdx.x % kWave);
 }
 
-// Lanes that are `on` and hold the same digit.
+// Lanes that are `on` and hold the same digit: for each bit, those whose bit
+// is this lane's (its sign over a word turns the ballot around).
 __device__ __forceinline__ uint64_t same_digit(int digit, bool on, int digit_bits) {
-  uint64_t same = wave_ballot(on);
-  for (int b = 0; b < digit_bits; ++b) {
-    const bool bit = (digit >> b) & 1;
-    const uint64_t m = wave_ballot(bit);
-    same &= bit ? m : ~m;
+  const uint64_t all = wave_ballot(on);
+  uint32_t lo = (uint32_t)all, hi = (uint32_t)(all >> 32);
+#pragma unroll
+  for (int b = 0; b < kSortBits; ++b) {
+    if (b >= digit_bits) break;
+    const uint32_t bit = (uint32_t)((int32_t)((uint32_t)digit << (31 - b)) >> 31);
+    const uint64_t m = wave_ballot(bit != 0);
+    lo &= ~((uint32_t)m ^ bit);
+    hi &= ~((uint32_t)(m >> 32) ^ bit);
   }
-  return same;
+  return lo | (uint64_t)hi << 32;
 }
 
 // rank[r]: the number of equal digits in earlier slots of the wave; cnt[w][d]:

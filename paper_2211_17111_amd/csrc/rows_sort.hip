@@ -7,8 +7,8 @@
 // per digit bit finds the lanes of equal digit) and counters per wave and digit,
 // all in slot order: the sort is stable and every result the same on every run.
 //
-// Up to 4096 slots one workgroup does all passes in LDS.  More slots are cut
-// into tiles of 1024, eight to a group, and every pass is
+// Up to 4096 slots, and up to 8192 that take several passes, one workgroup does
+// all passes in LDS.  More slots are cut into tiles of 1024, eight to a group, and every pass is
 //   hist      per group, the digit counts of its tiles, summed over the tiles
 //             before each, and the group's counts
 //   (scan     per digit, the sum over the groups before each group, and over
@@ -23,10 +23,10 @@
 // Microseconds per sort, launches back to back in a graph, with 128 and with
 // 131,072 keys (two passes and the search):
 //   slots            64   1024   4096   8192  16384  131072  1000000
-//   128 keys        4.1    4.6    7.8    9.2    9.5    10.3     24.7
-//   131,072 keys    9.4   11.7   21.4   26.9   28.5    33.9     88.3
-// One workgroup takes 12.9 and 34.5 at 8192 slots, and tiles 8.6 and 24.5 at
-// 4097: hence the border at 4096.
+//   128 keys        4.0    4.6    6.9    9.1    9.5    10.2     24.7
+//   131,072 keys    8.9   10.8   16.5   24.2   28.5    33.9     88.8
+// At 8192 slots one workgroup takes 10.6 with 128 keys, and tiles take 26.9 with
+// 131,072.
 
 #include <algorithm>
 
@@ -159,11 +159,13 @@ __global__ __launch_bounds__(kTileThreads) void k_keys_scatter(
     const int d = threadIdx.x * per + q;
     if (q >= per || d >= digits) continue;
     int at = start + before[q];
+    int c[kTileWaves];
+#pragma unroll
+    for (int w = 0; w < kTileWaves; ++w) c[w] = cnt[w][d];
 #pragma unroll
     for (int w = 0; w < kTileWaves; ++w) {
-      const int c = cnt[w][d];
       cnt[w][d] = at;
-      at += c;
+      at += c[w];
     }
     if (offsets != nullptr && blockIdx.x == 0 && d <= n_keys) offsets[d] = start;
     start += tot[q];
@@ -179,30 +181,29 @@ __global__ __launch_bounds__(kTileThreads) void k_keys_scatter(
   }
 }
 
-// All passes over at most kSmallSort slots in one workgroup.
+// All passes over at most ROUNDS * 1024 slots in one workgroup.
 constexpr int kSmallThreads = 1024;
 constexpr int kSmallWaves = kSmallThreads / kWave;
-constexpr int kSmallRounds = kSmallSort / kSmallThreads;
 
-template <typename TKey>
+template <typename TKey, int ROUNDS>
 __global__ __launch_bounds__(kSmallThreads) void k_keys_small(
     const TKey* __restrict__ keys, int32_t n, int32_t n_keys, int passes, int digit_bits,
     int32_t* __restrict__ order, int32_t* __restrict__ position, int32_t* __restrict__ offsets,
     int32_t* __restrict__ sorted_keys) {
-  __shared__ uint16_t cnt[kSmallWaves][kMaxDigits];  // (a wave has at most 256 slots)
+  __shared__ __attribute__((aligned(4))) uint16_t cnt[kSmallWaves][kMaxDigits];  // (a wave has few slots)
   __shared__ int32_t s_start[kMaxDigits];
   __shared__ int s_scan[kSmallWaves];
-  __shared__ int32_t s_key[kSmallSort];
-  __shared__ uint16_t s_slot[kSmallSort];
+  __shared__ int32_t s_key[ROUNDS * kSmallThreads];
+  __shared__ uint16_t s_slot[ROUNDS * kSmallThreads], s_pos[ROUNDS * kSmallThreads];
   const int t = threadIdx.x;
   const int wid = t / kWave, lane = t % kWave;
   const int digits = 1 << digit_bits;
   const int rounds = (n + kSmallThreads - 1) / kSmallThreads;
   const int base = wid * rounds * kWave + lane;  // the wave's slots are consecutive
-  int32_t key[kSmallRounds];
-  uint32_t slot[kSmallRounds];
+  int32_t key[ROUNDS];
+  uint32_t slot[ROUNDS];
 #pragma unroll
-  for (int r = 0; r < kSmallRounds; ++r) {
+  for (int r = 0; r < ROUNDS; ++r) {
     const int i = base + r * kWave;
     const bool on = r < rounds && i < n;
     key[r] = on ? key_or_drop(keys, i, n_keys) : 0;
@@ -210,21 +211,21 @@ __global__ __launch_bounds__(kSmallThreads) void k_keys_small(
   }
   for (int p = 0; p < passes; ++p) {
     const int shift = p * digit_bits;
-    for (int w = 0; w < kSmallWaves; ++w)
-      for (int d = t; d < digits; d += kSmallThreads) cnt[w][d] = 0;
+    for (int i = t; i < kSmallWaves * kMaxDigits / 2; i += kSmallThreads)
+      reinterpret_cast<uint32_t*>(cnt)[i] = 0;
     lds_barrier();
     if (p > 0) {
 #pragma unroll
-      for (int r = 0; r < kSmallRounds; ++r) {
+      for (int r = 0; r < ROUNDS; ++r) {
         const int i = base + r * kWave;
         if (r >= rounds || i >= n) continue;
         key[r] = s_key[i];
         slot[r] = s_slot[i];
       }
     }
-    int32_t rank[kSmallRounds];
+    int32_t rank[ROUNDS];
 #pragma unroll
-    for (int r = 0; r < kSmallRounds; ++r) {
+    for (int r = 0; r < ROUNDS; ++r) {
       rank[r] = 0;
       if (r >= rounds) continue;  // (uniform)
       const bool on = base + r * kWave < n;
@@ -237,12 +238,16 @@ __global__ __launch_bounds__(kSmallThreads) void k_keys_small(
     }
     lds_barrier();
     int tot = 0;  // digit t: the waves' offsets within the digit, and its count
-    if (t < digits)
+    if (t < digits) {
+      int c[kSmallWaves];
+#pragma unroll
+      for (int w = 0; w < kSmallWaves; ++w) c[w] = cnt[w][t];
+#pragma unroll
       for (int w = 0; w < kSmallWaves; ++w) {
-        const int c = cnt[w][t];
         cnt[w][t] = (uint16_t)tot;
-        tot += c;
+        tot += c[w];
       }
+    }
     int all;
     const int start = block_exclusive_scan<kSmallThreads, true>(tot, s_scan, &all);
     if (t < digits) s_start[t] = start;
@@ -250,20 +255,21 @@ __global__ __launch_bounds__(kSmallThreads) void k_keys_small(
     lds_barrier();
     const bool last = p == passes - 1;
 #pragma unroll
-    for (int r = 0; r < kSmallRounds; ++r) {
+    for (int r = 0; r < ROUNDS; ++r) {
       if (r >= rounds || base + r * kWave >= n) continue;
       const int digit = (key[r] >> shift) & (digits - 1);
       const int pos = s_start[digit] + cnt[wid][digit] + rank[r];
-      if (last) {
-        order[pos] = (int32_t)slot[r];
-        if (position != nullptr) position[slot[r]] = pos;
-        if (sorted_keys != nullptr) sorted_keys[pos] = key[r];
-      } else {
-        s_key[pos] = key[r];
-        s_slot[pos] = (uint16_t)slot[r];
-      }
+      s_key[pos] = key[r];
+      s_slot[pos] = (uint16_t)slot[r];
+      if (last) s_pos[slot[r]] = (uint16_t)pos;
     }
     lds_barrier();
+  }
+  // (out of LDS in order: one unit's scattered stores took 5 us for 4096 slots)
+  for (int i = t; i < n; i += kSmallThreads) {
+    order[i] = s_slot[i];
+    if (position != nullptr) position[i] = s_pos[i];
+    if (sorted_keys != nullptr) sorted_keys[i] = s_key[i];
   }
 }
 
@@ -291,7 +297,8 @@ SortLayout sort_layout(int64_t n, int64_t n_keys) {
     off += (sizeof(int32_t) * (size_t)ints + 255) & ~size_t(255);
     return o;
   };
-  if (n > kSmallSort) {
+  L.small = n <= (L.passes > 1 ? kSmallSortPasses : kSmallSort);
+  if (!L.small) {
     L.tile_counts = take((L.groups * kGroupTiles) << L.digit_bits);
     L.group_counts = take(L.groups << L.digit_bits);
     L.totals = take(int64_t(1) << L.digit_bits);
@@ -319,11 +326,16 @@ hipError_t launch_sort_keys(int64_t n, int64_t n_keys, int key_type, const void*
   char* ws = static_cast<char*>(workspace);
   auto W = [&](size_t o) { return reinterpret_cast<int32_t*>(ws + o); };
   const int32_t nk = (int32_t)n_keys;
-  if (n <= kSmallSort) {
+  if (L.small) {
     int32_t* sorted = sorted_keys != nullptr ? sorted_keys : L.passes > 1 ? W(L.keys[0]) : nullptr;
+    auto run = [&](auto* k, auto rounds) {
+      k_keys_small<std::remove_const_t<std::remove_pointer_t<decltype(k)>>, rounds.value>
+          <<<1, kSmallThreads, 0, stream>>>(k, (int32_t)n, nk, L.passes, L.digit_bits, order,
+                                            position, offsets, sorted);
+    };
     auto go = [&](auto* k) {
-      k_keys_small<<<1, kSmallThreads, 0, stream>>>(k, (int32_t)n, nk, L.passes, L.digit_bits,
-                                                    order, position, offsets, sorted);
+      if (n <= kSmallSort) run(k, std::integral_constant<int, kSmallSort / kSmallThreads>{});
+      else run(k, std::integral_constant<int, kSmallSortPasses / kSmallThreads>{});
     };
     if (key_type == BEVPOOL_KEY_I64) go(static_cast<const int64_t*>(keys));
     else go(static_cast<const int32_t*>(keys));

@@ -70,7 +70,8 @@ def _keys(n, n_keys, seed, kind="even"):
 
 # ------------------------------------------------------------------- sorting
 
-@pytest.mark.parametrize("n", [0, 1, 2, 63, 64, 65, 255, 257, 1000, 2047, 2048, 2049, 4097, 8191, 70001])
+@pytest.mark.parametrize("n", [0, 1, 2, 63, 64, 65, 255, 257, 1000, 2047, 2048, 2049, 4096, 4097, 8191, 8192, 8193,
+                               70001])
 @pytest.mark.parametrize("n_keys", [1, 2, 7, 255, 256, 1023, 1024, 5000, (1 << 20) + 3])
 def test_sort_keys(n, n_keys):
     say(f"sort_keys n={n} n_keys={n_keys}")

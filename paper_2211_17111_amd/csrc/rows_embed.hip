@@ -43,13 +43,14 @@ __global__ __launch_bounds__(kRowThreads) void k_embed(const T* __restrict__ tab
 //                   is that range's partial 2 r, of one that starts here and
 //                   goes on into the next 2 r + 1 (float32 rows).
 //   k_embed_rest    blocks of ids fill the rows of ids that do not occur;
-//                   blocks of ranges add up, in range order within each of
-//                   their lane groups and then over the groups, the partials
-//                   of the id that starts in the range and goes on.
+//                   lane groups, one to a range, add up the partials of the id
+//                   that starts in the range and goes on, in range order; the
+//                   block's groups share an id of many partials and add their
+//                   sums in group order.
 //
 // Measured with 16,384 ids of a text (the most frequent 917 times) and a
-// bfloat16 table of 131072 x 4096 (1.07 GB): ranges 64 us, rest 175 us (its fill
-// runs at 5.9 TB/s), where one owner per table row took 1866 us.
+// bfloat16 table of 131072 x 4096 (1.07 GB): ranges 44 us, rest 171 us (its fill
+// runs at 6.0 TB/s), where one owner per table row took 1866 us.
 struct Ranges {
   const int32_t* order;
   const int32_t* keys;     // of the sorted slots
@@ -245,11 +246,11 @@ __global__ __launch_bounds__(kRowThreads) void k_embed_rest(RowSplit s, Ranges a
 // are 8,192, then longer ones; and up to a third of an id's mean count, at most
 // 64, where every id has many slots to join.  Microseconds of the whole
 // gradient (with its sort) with ranges of 8, 16, 32, 64 and 128 slots:
-//   16,384 slots, 131,072 ids (text), C = 4096, bfloat16   290  281  275  286  332  (takes 16)
-//   130,160 slots, 16,384 ids (even), C = 80, float32       75   68   70   81  107  (16)
-//   2,048 slots, 32,000 ids (text), C = 1024, bfloat16      51   55   63   79  111  (8)
-//   65,536 slots, 1,000 ids (even), C = 1024, bfloat16      73   60   52   57   76  (32)
-//   65,536 slots, 3 ids, C = 512, float32                  143   94   65   59   73  (64)
+//   16,384 slots, 131,072 ids (text), C = 4096, bfloat16   272  268  266  284  319  (takes 16)
+//   130,160 slots, 16,384 ids (even), C = 80, float32       44   43   50   63   90  (16)
+//   2,048 slots, 32,000 ids (text), C = 1024, bfloat16      27   31   39   56   88  (8)
+//   65,536 slots, 1,000 ids (even), C = 1024, bfloat16      68   61   55   67   95  (32)
+//   65,536 slots, 3 ids, C = 512, float32                  177  112   78   75   97  (64)
 int32_t range_slots(int64_t n, int64_t n_keys, int64_t C) {
   const int64_t tiles = (C + 511) / 512;
   int32_t RG = 8;

@@ -7,6 +7,7 @@ Python binding loads it.
 
 from __future__ import annotations
 
+import fcntl
 import os
 import subprocess
 import sys
@@ -135,6 +136,12 @@ def build_sanitized(verbose: bool = False) -> str:
     ABI tests' argument-validation paths (no GPU needed).  Rebuilt only when
     a source or header is newer than it."""
     os.makedirs(SAN_DIR, exist_ok=True)
+    with open(os.path.join(SAN_DIR, "lock"), "w") as lock:  # (two test processes may ask at once)
+        fcntl.flock(lock, fcntl.LOCK_EX)
+        return _build_sanitized(verbose)
+
+
+def _build_sanitized(verbose: bool) -> str:
     inputs = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(INCLUDE, f) for f in os.listdir(INCLUDE)]
     if os.path.exists(SAN_LIB) and os.path.getmtime(SAN_LIB) >= max(map(os.path.getmtime, inputs)):
         return SAN_LIB

@@ -290,9 +290,9 @@ __global__ __launch_bounds__(kRowThreads) void k_combine_backward(
 
 // Lanes per token of the combine's gradient: no more than a row has vectors, a
 // whole block for rows that fill it (their k slots then go through DRAM in
-// whole rows: 16,384 tokens of 4 slots, C = 2048 in bfloat16, 130 us by waves
-// and 118 by blocks, before the rows were streamed: 111) and where waves would leave the device empty (fewer than
-// eight to a compute unit).
+// whole rows: 16,384 tokens of 4 slots, C = 2048 in bfloat16, took 130 us by
+// waves and 118 by blocks, and 111 since the rows are streamed) and where waves
+// would leave the device empty (fewer than eight to a compute unit).
 template <class F>
 void by_lanes(int64_t rows, int64_t cv, F f) {
   if (cv >= kRowThreads || (cv > kWave && rows < 2048))

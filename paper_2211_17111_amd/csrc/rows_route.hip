@@ -101,7 +101,8 @@ __device__ __forceinline__ bool group_any(bool v) {
 }
 
 // The logits of lane l: runs of B neighbours, so that a lane loads vectors and
-// the group's are next to each other.  Register i holds expert at(i).
+// the group's are next to each other.  Register i holds expert first(l) +
+// offset(i).
 template <typename T, int L, int V>
 struct Held {
   static constexpr int B = V < RowVec<T>::N ? V : RowVec<T>::N;

@@ -8,7 +8,8 @@
 // all in slot order: the sort is stable and every result the same on every run.
 //
 // Up to 4096 slots, and up to 8192 that take several passes, one workgroup does
-// all passes in LDS.  More slots are cut into tiles of 1024, eight to a group, and every pass is
+// all passes in LDS.  More slots are cut into tiles of 1024, eight to a group,
+// and every pass is
 //   hist      per group, the digit counts of its tiles, summed over the tiles
 //             before each, and the group's counts
 //   (scan     per digit, the sum over the groups before each group, and over

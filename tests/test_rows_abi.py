@@ -39,7 +39,8 @@ def test_header_is_c():
         pytest.skip("no host C compiler")
     inc = os.path.dirname(bp.HEADER_PATH)
     subprocess.run([gcc, "-std=c99", "-Wall", "-Werror", "-I", inc, "-x", "c", "-fsyntax-only", "-"],
-                   input=b'#include "bevpool_rows.h"\n', check=True)
+                   input=b'#include "bevpool_rows.h"\n', check=True,
+                   env={k: v for k, v in os.environ.items() if k != "LD_PRELOAD"})
     text = open(os.path.join(inc, "bevpool_rows.h")).read()
     assert int(re.search(r"#define BEVPOOL_BF16 (\d+)", text).group(1)) == rows.BEVPOOL_BF16
     for name in ("BEVPOOL_KEY_I32", "BEVPOOL_KEY_I64"):

@@ -149,28 +149,34 @@ def _elsewhere(dev: torch.device, stream, *inputs):
 class KeyOrder:
     """Stable order of n slots by key: ``order[q]`` the slot at place q,
     ``position[s]`` the place of slot s, ``offsets[v]`` the first place of key
-    v, ``offsets[n_keys]`` the number of kept slots (dropped ones lie behind)."""
+    v, ``offsets[n_keys]`` the number of kept slots (dropped ones lie behind).
+    ``k``: the slots of a token, where the keys were a matrix."""
     order: torch.Tensor
     position: torch.Tensor
     offsets: torch.Tensor
     n_keys: int
+    k: int | None = None
 
-    def _check(self, dev: torch.device, n: int) -> int:
-        """Address of the number of kept slots."""
+    def _check(self, dev: torch.device, n: int, k: int) -> int:
+        """Address of the number of kept slots, of n slots, k to a token."""
         position, offsets, n_keys = self.position, self.offsets, self.n_keys
         _dense(position, "position", dev, _I32)
         _dense(offsets, "offsets", dev, _I32)
         if position.numel() != n or offsets.numel() != n_keys + 1:
             raise ValueError(f"the order has {position.numel()} slots and {offsets.numel()} offsets; "
                              f"{n} slots and {n_keys + 1} offsets are needed")
+        if self.k is not None and self.k != k and n > 0:
+            raise ValueError(f"the order has {self.k} slots to a token, not {k}")
         return offsets.data_ptr() + 4 * n_keys
 
 
-def _key_order(n: int, n_keys: int, dev: torch.device):
+def _key_order(keys: torch.Tensor, n_keys: int, dev: torch.device):
+    n = keys.numel()
     nbytes = _size("bevpool_sort_keys_workspace_size", n, n_keys)
     i32 = torch.int32
     plan = KeyOrder(torch.empty(n, dtype=i32, device=dev), torch.empty(n, dtype=i32, device=dev),
-                    torch.empty(n_keys + 1, dtype=i32, device=dev), n_keys)
+                    torch.empty(n_keys + 1, dtype=i32, device=dev), n_keys,
+                    keys.shape[1] if keys.dim() == 2 else None)
     return plan, torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None, nbytes
 
 
@@ -185,9 +191,8 @@ def sort_keys(keys: torch.Tensor, n_keys: int, stream=None) -> KeyOrder:
     if ctx is not None:
         with ctx:
             return sort_keys(keys, n_keys)
-    n = keys.numel()
-    plan, ws, nbytes = _key_order(n, n_keys, dev)
-    _call("bevpool_sort_keys", n, n_keys, _KEY_CODE[keys.dtype], keys.data_ptr(), plan.order.data_ptr(),
+    plan, ws, nbytes = _key_order(keys, n_keys, dev)
+    _call("bevpool_sort_keys", keys.numel(), n_keys, _KEY_CODE[keys.dtype], keys.data_ptr(), plan.order.data_ptr(),
           plan.position.data_ptr(), plan.offsets.data_ptr(), _bp._ptr(ws), nbytes, _stream(dev))
     return plan
 
@@ -247,7 +252,7 @@ def dispatch_forward(x: torch.Tensor, ids, n_experts: int | None = None, stream=
         plan = ids
         n = plan.position.numel()
         k = n // T if T else 1
-        kept = plan._check(dev, T * k)
+        kept = plan._check(dev, T * k, k)
     else:
         _dense(ids, "ids", dev, _KEY_CODE)
         if ids.dim() != 2 or ids.shape[0] != T:
@@ -265,7 +270,7 @@ def dispatch_forward(x: torch.Tensor, ids, n_experts: int | None = None, stream=
         _call("bevpool_dispatch_rows", T, k, C, _DTYPE_CODE[x.dtype], x.data_ptr(), stride, plan.position.data_ptr(),
               kept, out.data_ptr(), _stream(dev))
         return out, plan
-    plan, ws, nbytes = _key_order(n, n_experts, dev)
+    plan, ws, nbytes = _key_order(ids, n_experts, dev)
     _call("bevpool_dispatch_forward", T, k, C, n_experts, _DTYPE_CODE[x.dtype], x.data_ptr(), stride,
           _KEY_CODE[ids.dtype], ids.data_ptr(), plan.order.data_ptr(), plan.position.data_ptr(),
           plan.offsets.data_ptr(), out.data_ptr(), _bp._ptr(ws), nbytes, _stream(dev))
@@ -283,7 +288,7 @@ def dispatch_backward(grad_rows: torch.Tensor, plan: KeyOrder, k: int, stream=No
     dev = _device(grad_rows, "grad_rows")
     stride = _matrix(grad_rows, "grad_rows", dev)
     T = _tokens(grad_rows, k)
-    kept = plan._check(dev, T * k)
+    kept = plan._check(dev, T * k, k)
     ctx = _elsewhere(dev, stream, grad_rows, plan.position, plan.offsets)
     if ctx is not None:
         with ctx:
@@ -307,7 +312,7 @@ def combine_forward(rows: torch.Tensor, weights: torch.Tensor, plan: KeyOrder, o
     if weights.dim() != 2 or weights.numel() != n:
         raise ValueError(f"weights must be (T, k) for {n} rows, got {tuple(weights.shape)}")
     T, k = weights.shape
-    kept = plan._check(dev, n)
+    kept = plan._check(dev, n, k)
     odt = out_dtype or rows.dtype
     if odt not in (rows.dtype, torch.float32):
         raise ValueError(f"out_dtype must be {rows.dtype} or float32, got {odt}")
@@ -336,7 +341,7 @@ def combine_backward(grad_out: torch.Tensor, rows: torch.Tensor, weights: torch.
     grad_stride = _matrix(grad_out, "grad_out", dev, shape=(T, C))
     if grad_out.dtype not in (rows.dtype, torch.float32):
         raise ValueError(f"grad_out must be {rows.dtype} or float32, got {grad_out.dtype}")
-    kept = plan._check(dev, n)
+    kept = plan._check(dev, n, k)
     ctx = _elsewhere(dev, stream, grad_out, rows, weights, plan.position, plan.offsets)
     if ctx is not None:
         with ctx:
@@ -500,7 +505,7 @@ def dispatch(x: torch.Tensor, ids, n_experts: int | None = None):
     if isinstance(ids, KeyOrder):
         return DispatchFunction.apply(x, ids, None), ids
     rows, order, position, offsets = DispatchFunction.apply(x, ids, n_experts)
-    return rows, KeyOrder(order, position, offsets, n_experts)
+    return rows, KeyOrder(order, position, offsets, n_experts, ids.shape[1])
 
 
 def combine(rows: torch.Tensor, weights: torch.Tensor, plan: KeyOrder, out_dtype=None) -> torch.Tensor:

@@ -683,6 +683,10 @@ def test_refusals():
         lambda: rows.combine_forward(y, w.half(), plan),
         lambda: rows.combine_forward(y, w, plan, F16),
         lambda: rows.combine_forward(y[:8], w[:4], plan),
+        lambda: rows.combine_forward(y, w.view(4, 4), plan),  # as many slots, otherwise grouped
+        lambda: rows.dispatch_backward(y, plan, 4),
+        lambda: rows.dispatch_forward(x[:4], plan),
+        lambda: rows.combine_backward(x[:4], y, w.view(4, 4), plan),
         lambda: rows.combine_backward(x[:, :8], y, w, plan),
         lambda: rows.combine_backward(x.half(), y, w, plan),
         lambda: rows.combine_backward(x, y, w.cpu(), plan),

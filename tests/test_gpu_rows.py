@@ -485,8 +485,9 @@ def test_expert_layer_on_embedded_tokens():
     p = p / p.sum(1, keepdim=True)
     out64 = torch.einsum("te,td,edc->tc", p, x64, m64)
     (out64 * target.double().cpu()).sum().backward()
-    # float32 through products of length C and softmaxes of logits of size 30: relative to the
-    # tensor's largest value, 2^-24 x (2 C + 4 |logit| + ...) with room for the matrix products
+    # A logit is a sum of C = 24 products of magnitude 60 in all at most, so it is off by at most
+    # 26 x 60 x 2^-24, and a weight by that relative to itself; the experts' products and the sums of
+    # their gradients add (C + 2) 2^-24 each: 2000 x 2^-24 of the tensor's largest value covers them.
     for a, b in ((out, out64), (table.grad, t64.grad), (wr.grad, r64.grad), (w1.grad, m64.grad)):
         err = (a.detach().double().cpu() - b.detach()).abs().max()
         assert err <= 2000 * U * b.detach().abs().max(), float(err / b.detach().abs().max())

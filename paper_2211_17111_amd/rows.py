@@ -162,6 +162,8 @@ class KeyOrder:
         position, offsets, n_keys = self.position, self.offsets, self.n_keys
         _dense(position, "position", dev, _I32)
         _dense(offsets, "offsets", dev, _I32)
+        if n_keys < 0:  # (the count would lie before the offsets)
+            raise ValueError(f"n_keys = {n_keys} is negative")
         if position.numel() != n or offsets.numel() != n_keys + 1:
             raise ValueError(f"the order has {position.numel()} slots and {offsets.numel()} offsets; "
                              f"{n} slots and {n_keys + 1} offsets are needed")

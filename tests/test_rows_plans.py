@@ -1,0 +1,24 @@
+"""What a KeyOrder given by the caller has to hold before its addresses reach a
+kernel (no GPU: the checks look at shapes only)."""
+
+import pytest
+import torch
+
+from paper_2211_17111_amd import rows
+
+CPU, META = torch.device("cpu"), torch.device("meta")
+
+
+def _i32(n, dev=CPU):
+    return torch.empty(n, dtype=torch.int32, device=dev)
+
+
+def test_count_of_kept_slots_lies_inside_the_offsets():
+    """offsets[n_keys] is read on the device: n_keys must name an element of them."""
+    offsets = _i32(4)
+    assert rows.KeyOrder(_i32(6), _i32(6), offsets, 3)._check(CPU, 6, 2) == offsets.data_ptr() + 12
+    assert rows.KeyOrder(_i32(0), _i32(0), _i32(1), 0)._check(CPU, 0, 1) != 0
+    for n in (0, 6):
+        for n_keys in (-1, -2):
+            with pytest.raises(ValueError):
+                rows.KeyOrder(_i32(n), _i32(n), _i32(max(0, n_keys + 1)), n_keys)._check(CPU, n, 1)

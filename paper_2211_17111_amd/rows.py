@@ -130,6 +130,16 @@ def _dense(t, name: str, dev: torch.device, dtypes, shape=None) -> None:
         raise ValueError(f"{name} must be contiguous")
 
 
+# The library's counts of experts, of choices and of slots to a token are 32-bit
+# integers, of which a larger one would pass its low bits only.
+_LIMIT = 1 << 31
+
+
+def _check_choices(E: int, k: int) -> None:
+    if E >= _LIMIT or k >= _LIMIT:
+        raise ValueError(f"{k} of {E} experts exceed 2^31 - 1")
+
+
 def _elsewhere(dev: torch.device, stream, *inputs):
     """A context in which dev and `stream` are current, or None where they
     already are: allocations and launches then belong to that stream."""
@@ -167,6 +177,8 @@ class KeyOrder:
         if position.numel() != n or offsets.numel() != n_keys + 1:
             raise ValueError(f"the order has {position.numel()} slots and {offsets.numel()} offsets; "
                              f"{n} slots and {n_keys + 1} offsets are needed")
+        if n >= _LIMIT:
+            raise ValueError(f"{n} slots exceed 2^31 - 1")
         if self.k is not None and self.k != k and n > 0:
             raise ValueError(f"the order has {self.k} slots to a token, not {k}")
         return offsets.data_ptr() + 4 * n_keys
@@ -208,11 +220,12 @@ def route_forward(logits: torch.Tensor, k: int, renormalise: bool = True, stream
     (renormalise) or over all experts."""
     dev = _device(logits, "logits")
     stride = _matrix(logits, "logits", dev)
+    T, E = logits.shape
+    _check_choices(E, k)
     ctx = _elsewhere(dev, stream, logits)
     if ctx is not None:
         with ctx:
             return route_forward(logits, k, renormalise)
-    T, E = logits.shape
     weights = torch.empty((T, k), dtype=torch.float32, device=dev)
     ids = torch.empty((T, k), dtype=torch.int32, device=dev)
     _call("bevpool_route_forward", T, E, k, _DTYPE_CODE[logits.dtype], logits.data_ptr(), stride, int(renormalise),
@@ -227,6 +240,7 @@ def route_backward(grad_weights: torch.Tensor, logits: torch.Tensor, weights: to
     stride = _matrix(logits, "logits", dev)
     T, E = logits.shape
     k = ids.shape[-1]
+    _check_choices(E, k)
     _dense(grad_weights, "grad_weights", dev, _F32, (T, k))
     _dense(weights, "weights", dev, _F32, (T, k))
     _dense(ids, "ids", dev, _I32, (T, k))

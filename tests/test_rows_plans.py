@@ -22,3 +22,11 @@ def test_count_of_kept_slots_lies_inside_the_offsets():
         for n_keys in (-1, -2):
             with pytest.raises(ValueError):
                 rows.KeyOrder(_i32(n), _i32(n), _i32(max(0, n_keys + 1)), n_keys)._check(CPU, n, 1)
+
+
+def test_orders_past_32_bits_are_refused():
+    """Slots and slots to a token reach the library as 32-bit integers."""
+    n = 1 << 32
+    for k in (1, n):
+        with pytest.raises(ValueError):
+            rows.KeyOrder(_i32(n, META), _i32(n, META), _i32(4, META), 3)._check(META, n, k)

@@ -160,7 +160,7 @@ class KeyOrder:
     """Stable order of n slots by key: ``order[q]`` the slot at place q,
     ``position[s]`` the place of slot s, ``offsets[v]`` the first place of key
     v, ``offsets[n_keys]`` the number of kept slots (dropped ones lie behind).
-    ``k``: the slots of a token, where the keys were a matrix."""
+    ``k``: the slots of a token, where a dispatch made the order."""
     order: torch.Tensor
     position: torch.Tensor
     offsets: torch.Tensor
@@ -184,13 +184,12 @@ class KeyOrder:
         return offsets.data_ptr() + 4 * n_keys
 
 
-def _key_order(keys: torch.Tensor, n_keys: int, dev: torch.device):
+def _key_order(keys: torch.Tensor, n_keys: int, dev: torch.device, k: int | None = None):
     n = keys.numel()
     nbytes = _size("bevpool_sort_keys_workspace_size", n, n_keys)
     i32 = torch.int32
     plan = KeyOrder(torch.empty(n, dtype=i32, device=dev), torch.empty(n, dtype=i32, device=dev),
-                    torch.empty(n_keys + 1, dtype=i32, device=dev), n_keys,
-                    keys.shape[1] if keys.dim() == 2 else None)
+                    torch.empty(n_keys + 1, dtype=i32, device=dev), n_keys, k)
     return plan, torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None, nbytes
 
 
@@ -198,7 +197,8 @@ def _key_order(keys: torch.Tensor, n_keys: int, dev: torch.device):
 
 def sort_keys(keys: torch.Tensor, n_keys: int, stream=None) -> KeyOrder:
     """Stable order of integer keys (any shape, int32 or int64) in [0, n_keys);
-    keys outside are dropped."""
+    keys outside are dropped.  A key is a slot; how many of them make a token is
+    the caller's to say, by the rows that go through the order."""
     dev = _device(keys, "keys")
     _dense(keys, "keys", dev, _KEY_CODE)
     ctx = _elsewhere(dev, stream, keys)
@@ -286,7 +286,7 @@ def dispatch_forward(x: torch.Tensor, ids, n_experts: int | None = None, stream=
         _call("bevpool_dispatch_rows", T, k, C, _DTYPE_CODE[x.dtype], x.data_ptr(), stride, plan.position.data_ptr(),
               kept, out.data_ptr(), _stream(dev))
         return out, plan
-    plan, ws, nbytes = _key_order(ids, n_experts, dev)
+    plan, ws, nbytes = _key_order(ids, n_experts, dev, k)
     _call("bevpool_dispatch_forward", T, k, C, n_experts, _DTYPE_CODE[x.dtype], x.data_ptr(), stride,
           _KEY_CODE[ids.dtype], ids.data_ptr(), plan.order.data_ptr(), plan.position.data_ptr(),
           plan.offsets.data_ptr(), out.data_ptr(), _bp._ptr(ws), nbytes, _stream(dev))

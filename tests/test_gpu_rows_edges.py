@@ -27,3 +27,26 @@ def test_counts_past_32_bits_are_refused():
               lambda: rows.route_backward(many_w, x[:0], many_w, many_ids)):
         with pytest.raises(ValueError):
             f()
+
+
+# --------------------------------------------------------------------- plans
+
+def test_order_of_a_matrix_of_ids():
+    """sort_keys takes any shape: its plan serves one slot to a token and rows of slots alike."""
+    B, S, E, C = 7, 5, 6, 24
+    keys = _ids(B, S, E, 4)
+    ids = torch.from_numpy(keys).to(DEV)
+    plan = rows.sort_keys(ids, E)
+    for T, k in ((B * S, 1), (B, S)):
+        x, g, w = _normal(T, C, seed=1), _normal(T * k, C, seed=2), _normal(T, k, seed=3)
+        got, same = rows.dispatch_forward(x, plan)
+        want, wplan = ref.dispatch_ref(_np(x), keys.reshape(T, k), E)
+        assert same is plan and np.array_equal(_np(got), want)
+        _same_plan(plan, wplan)
+        want, mag = ref.combine_ref(_np(g), np.ones((T, k)), wplan)
+        _near(rows.dispatch_backward(g, plan, k), want, (k + 2) * U * mag + _half_step(want, F32), f"k={k}")
+        want, mag = ref.combine_ref(_np(g), _np(w), wplan)
+        _near(rows.combine_forward(g, w, plan), want, (k + 2) * U * mag + _half_step(want, F32), f"combine k={k}")
+        leaf = x.clone().requires_grad_()
+        rows.dispatch(leaf, plan)[0].backward(g)
+        assert torch.equal(leaf.grad, rows.dispatch_backward(g, plan, k))

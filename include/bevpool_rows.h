@@ -80,7 +80,8 @@ int bevpool_sort_keys(int64_t n, int64_t n_keys, int key_type, const void* keys,
  *   renormalise: grad[id_j] = w_j (g_j - s), 0 elsewhere;
  *   else:        grad[e] = p_e (G_e - s), p the softmax over all experts and
  *                G_{id_j} = g_j, 0 elsewhere;  s = sum_j w_j g_j.
- * Slots with id -1 have no gradient.  The logits are only read when
+ * Slots whose id names no expert (-1, or outside [0, n_experts)) have no
+ * gradient and no part in s.  The logits are only read when
  * renormalise is 0 (else they may be NULL).
  */
 int bevpool_route_forward(int64_t rows, int32_t n_experts, int32_t k, int dtype,

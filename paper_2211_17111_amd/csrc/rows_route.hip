@@ -337,6 +337,7 @@ __global__ __launch_bounds__(kThreads) void k_route_backward(
     for (int q = 0; q < Q; ++q) {
       const int j = q * L + lane;
       id[q] = j < k ? ids[row * k + j] : -1;
+      if (id[q] >= E) id[q] = -1;  // (names no expert, like a negative one)
       w[q] = j < k ? weights[row * k + j] : 0.f;
       g[q] = j < k ? grad_weights[row * k + j] : 0.f;
       if (id[q] >= 0) s += w[q] * g[q];
@@ -347,7 +348,7 @@ __global__ __launch_bounds__(kThreads) void k_route_backward(
     wave_lds_fence();
 #pragma unroll
     for (int q = 0; q < Q; ++q)
-      if (id[q] >= 0 && id[q] < E) {
+      if (id[q] >= 0) {
         const int run = id[q] / H::B;  // expert -> (lane, register)
         const int i = run / L * H::B + id[q] % H::B;
         mine[i * L + run % L] = renormalise ? w[q] * (g[q] - s) : g[q];

@@ -50,3 +50,17 @@ def test_order_of_a_matrix_of_ids():
         leaf = x.clone().requires_grad_()
         rows.dispatch(leaf, plan)[0].backward(g)
         assert torch.equal(leaf.grad, rows.dispatch_backward(g, plan, k))
+
+
+@pytest.mark.parametrize("renormalise", [True, False])
+def test_route_gradient_of_ids_outside(renormalise):
+    """An id that names no expert has no gradient, whichever side it lies on."""
+    T, E, k = 21, 20, 4
+    logits, g = plain._logits(T, E, F32, 1), _normal(T, k, seed=2)
+    w, ids = rows.route_forward(logits, k, renormalise)
+    outside = torch.rand((T, k), generator=torch.Generator().manual_seed(3)).to(DEV) < 0.4
+    outside[0], outside[1] = True, False
+    want = rows.route_backward(g, logits, w, torch.where(outside, -1, ids).int(), renormalise)
+    for v in (E, E + 9, (1 << 31) - 1, -(1 << 31)):
+        got = rows.route_backward(g, logits, w, torch.where(outside, v, ids).int(), renormalise)
+        assert torch.equal(got, want), v

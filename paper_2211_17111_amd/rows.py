@@ -237,7 +237,7 @@ def route_backward(grad_weights: torch.Tensor, logits: torch.Tensor, weights: to
                    renormalise: bool = True, stream=None) -> torch.Tensor:
     """Gradient (T, E) of the logits, in their type."""
     dev = _device(logits, "logits")
-    stride = _matrix(logits, "logits", dev)
+    _matrix(logits, "logits", dev)
     T, E = logits.shape
     k = ids.shape[-1]
     _check_choices(E, k)
@@ -248,9 +248,17 @@ def route_backward(grad_weights: torch.Tensor, logits: torch.Tensor, weights: to
     if ctx is not None:
         with ctx:
             return route_backward(grad_weights, logits, weights, ids, renormalise)
-    grad = torch.empty((T, E), dtype=logits.dtype, device=dev)
-    _call("bevpool_route_backward", T, E, k, _DTYPE_CODE[logits.dtype], grad_weights.data_ptr(), logits.data_ptr(),
-          stride, weights.data_ptr(), ids.data_ptr(), int(renormalise), grad.data_ptr(), _stream(dev))
+    return _route_gradient(grad_weights, None if renormalise else logits, weights, ids, E, logits.dtype)
+
+
+def _route_gradient(grad_weights, logits, weights, ids, E: int, dtype: torch.dtype) -> torch.Tensor:
+    """route_backward without its checks; logits None: of renormalised weights, whose gradient does not read them."""
+    dev = ids.device
+    T, k = ids.shape
+    grad = torch.empty((T, E), dtype=dtype, device=dev)
+    _call("bevpool_route_backward", T, E, k, _DTYPE_CODE[dtype], grad_weights.data_ptr(), _bp._ptr(logits),
+          0 if logits is None else logits.stride(0), weights.data_ptr(), ids.data_ptr(), int(logits is None),
+          grad.data_ptr(), _stream(dev))
     return grad
 
 
@@ -432,8 +440,8 @@ class RouteFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, k, renormalise):
         weights, ids = route_forward(logits, k, renormalise)
-        ctx.renormalise = renormalise
-        ctx.save_for_backward(logits, weights, ids)
+        ctx.experts, ctx.dtype = logits.shape[1], logits.dtype
+        ctx.save_for_backward(None if renormalise else logits, weights, ids)
         ctx.mark_non_differentiable(ids)
         ctx.set_materialize_grads(False)
         return weights, ids
@@ -444,7 +452,7 @@ class RouteFunction(torch.autograd.Function):
         if grad_weights is None:
             return None, None, None
         logits, weights, ids = ctx.saved_tensors
-        return route_backward(grad_weights.contiguous(), logits, weights, ids, ctx.renormalise), None, None
+        return _route_gradient(grad_weights.contiguous(), logits, weights, ids, ctx.experts, ctx.dtype), None, None
 
 
 class DispatchFunction(torch.autograd.Function):

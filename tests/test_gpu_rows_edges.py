@@ -64,3 +64,25 @@ def test_route_gradient_of_ids_outside(renormalise):
     for v in (E, E + 9, (1 << 31) - 1, -(1 << 31)):
         got = rows.route_backward(g, logits, w, torch.where(outside, v, ids).int(), renormalise)
         assert torch.equal(got, want), v
+
+
+# ------------------------------------------------------ what gradients keep
+
+def test_route_keeps_no_logits_that_its_gradient_does_not_read():
+    logits, g = plain._logits(9, 20, BF16, 1), _normal(9, 4, seed=2)
+    for renormalise in (True, False):
+        leaf = logits.clone().requires_grad_()
+        l = leaf * 1
+        w, ids = rows.route(l, 4, renormalise)
+        want = rows.route_backward(g, logits, w.detach(), ids, renormalise)
+        w.backward(g, retain_graph=True)
+        assert leaf.grad.dtype == BF16 and torch.equal(leaf.grad, want)
+        with torch.no_grad():
+            l.zero_()  # (the buffer is used again)
+        if renormalise:
+            leaf.grad = None
+            w.backward(g)
+            assert torch.equal(leaf.grad, want)
+        else:  # the softmax over all experts is formed again from them
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                w.backward(g)

@@ -356,13 +356,13 @@ def combine_backward(grad_out: torch.Tensor, rows: torch.Tensor, weights: torch.
     """(grad_rows, grad_weights) of combine_forward, in the types of rows and
     weights; None for one that is not needed."""
     dev = _device(rows, "rows")
-    stride = _matrix(rows, "rows", dev)
+    _matrix(rows, "rows", dev)
     _dense(weights, "weights", dev, (torch.float32, rows.dtype))
     n, C = rows.shape
     if weights.dim() != 2 or weights.numel() != n:
         raise ValueError(f"weights must be (T, k) for {n} rows, got {tuple(weights.shape)}")
     T, k = weights.shape
-    grad_stride = _matrix(grad_out, "grad_out", dev, shape=(T, C))
+    _matrix(grad_out, "grad_out", dev, shape=(T, C))
     if grad_out.dtype not in (rows.dtype, torch.float32):
         raise ValueError(f"grad_out must be {rows.dtype} or float32, got {grad_out.dtype}")
     kept = plan._check(dev, n, k)
@@ -370,12 +370,22 @@ def combine_backward(grad_out: torch.Tensor, rows: torch.Tensor, weights: torch.
     if ctx is not None:
         with ctx:
             return combine_backward(grad_out, rows, weights, plan, need_rows, need_weights)
-    grad_rows = torch.empty((n, C), dtype=rows.dtype, device=dev) if need_rows else None
-    grad_weights = torch.empty((T, k), dtype=weights.dtype, device=dev) if need_weights else None
-    _call("bevpool_combine_backward", T, k, C, _DTYPE_CODE[rows.dtype], _DTYPE_CODE[grad_out.dtype],
-          _DTYPE_CODE[weights.dtype], grad_out.data_ptr(), grad_stride, rows.data_ptr(), stride, weights.data_ptr(),
-          plan.position.data_ptr(), kept, grad_rows.data_ptr() if need_rows else None,
-          grad_weights.data_ptr() if need_weights else None, _stream(dev))
+    return _combine_gradients(grad_out, rows if need_weights else None, weights if need_rows else None,
+                              plan.position, kept, (T, k), rows.dtype, weights.dtype)
+
+
+def _combine_gradients(grad_out, rows, weights, position, kept: int, shape, rows_dtype, weights_dtype):
+    """combine_backward without its checks (kept: the address of the count): the gradient of the rows where the
+    weights are given, that of the weights where the rows are (each reads the other operand only)."""
+    dev = grad_out.device
+    T, k = shape
+    C = grad_out.shape[1]
+    grad_rows = torch.empty((T * k, C), dtype=rows_dtype, device=dev) if weights is not None else None
+    grad_weights = torch.empty((T, k), dtype=weights_dtype, device=dev) if rows is not None else None
+    _call("bevpool_combine_backward", T, k, C, _DTYPE_CODE[rows_dtype], _DTYPE_CODE[grad_out.dtype],
+          _DTYPE_CODE[weights_dtype], grad_out.data_ptr(), grad_out.stride(0), _bp._ptr(rows),
+          0 if rows is None else rows.stride(0), _bp._ptr(weights), position.data_ptr(), kept, _bp._ptr(grad_rows),
+          _bp._ptr(grad_weights), _stream(dev))
     return grad_rows, grad_weights
 
 
@@ -481,8 +491,10 @@ class DispatchFunction(torch.autograd.Function):
 class CombineFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, rows, weights, plan, out_dtype):
-        ctx.n_keys = plan.n_keys
-        ctx.save_for_backward(rows, weights, plan.position, plan.offsets)
+        need_rows, need_weights = ctx.needs_input_grad[:2]
+        ctx.n_keys, ctx.shape, ctx.dtypes = plan.n_keys, weights.shape, (rows.dtype, weights.dtype)
+        ctx.save_for_backward(rows if need_weights else None, weights if need_rows else None, plan.position,
+                              plan.offsets)
         ctx.set_materialize_grads(False)
         return combine_forward(rows, weights, plan, out_dtype)
 
@@ -492,8 +504,11 @@ class CombineFunction(torch.autograd.Function):
         if grad_out is None:
             return None, None, None, None
         rows, weights, position, offsets = ctx.saved_tensors
-        plan = KeyOrder(position, position, offsets, ctx.n_keys)
-        return *combine_backward(_rows_apart(grad_out), rows, weights, plan, *ctx.needs_input_grad[:2]), None, None
+        need_rows, need_weights = ctx.needs_input_grad[:2]
+        grads = _combine_gradients(_rows_apart(grad_out), rows if need_weights else None,
+                                   weights if need_rows else None, position, offsets.data_ptr() + 4 * ctx.n_keys,
+                                   ctx.shape, *ctx.dtypes)
+        return *grads, None, None
 
 
 class EmbedFunction(torch.autograd.Function):

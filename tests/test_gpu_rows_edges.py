@@ -86,3 +86,34 @@ def test_route_keeps_no_logits_that_its_gradient_does_not_read():
         else:  # the softmax over all experts is formed again from them
             with pytest.raises(RuntimeError, match="modified by an inplace operation"):
                 w.backward(g)
+
+
+def test_combine_keeps_no_operand_that_its_gradients_do_not_read():
+    T, k, E, C = 13, 3, 5, 40
+    _, plan = rows.dispatch_forward(_normal(T, C), torch.from_numpy(_ids(T, k, E, 1)).to(DEV), E)
+    y0, w0, g = _normal(T * k, C, dtype=BF16, seed=1), _normal(T, k, seed=2), _normal(T, C, dtype=BF16, seed=3)
+    want = rows.combine_backward(g, y0, w0, plan)
+    for on in ((True, False), (False, True), (True, True)):
+        leaves = [t.clone().requires_grad_(r) for t, r in zip((y0, w0), on)]
+        used = [t * 1 for t in leaves]
+        out = rows.combine(*used, plan)
+        out.backward(g, retain_graph=True)
+        for t, r, v in zip(leaves, on, want):
+            assert (t.grad is None) == (not r)
+            if r:
+                assert t.grad.dtype == t.dtype and torch.equal(t.grad, v)
+                one, = torch.autograd.grad(out, t, g, retain_graph=True)
+                assert torch.equal(one, v)
+        with torch.no_grad():
+            for t, r in zip(used, on):
+                if r:
+                    t.zero_()  # (the operand whose own gradient is wanted is not read for it)
+        if on == (True, True):
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                out.backward(g)
+            continue
+        for t in leaves:
+            t.grad = None
+        out.backward(g)
+        for t, r, v in zip(leaves, on, want):
+            assert not r or torch.equal(t.grad, v)

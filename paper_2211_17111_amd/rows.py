@@ -160,8 +160,9 @@ class KeyOrder:
     """Stable order of n slots by key: ``order[q]`` the slot at place q,
     ``position[s]`` the place of slot s, ``offsets[v]`` the first place of key
     v, ``offsets[n_keys]`` the number of kept slots (dropped ones lie behind).
-    ``k``: the slots of a token, where a dispatch made the order."""
-    order: torch.Tensor
+    ``k``: the slots of a token, where a dispatch made the order.  The moves go
+    by position and offsets: ``order`` may be None."""
+    order: torch.Tensor | None
     position: torch.Tensor
     offsets: torch.Tensor
     n_keys: int
@@ -483,7 +484,7 @@ class DispatchFunction(torch.autograd.Function):
         if grad_rows is None:
             return None, None, None
         position, offsets = ctx.saved_tensors
-        plan = KeyOrder(position, position, offsets, ctx.n_keys)
+        plan = KeyOrder(None, position, offsets, ctx.n_keys)
         k = position.numel() // ctx.tokens if ctx.tokens else 1
         return dispatch_backward(_rows_apart(grad_rows), plan, k), None, None
 

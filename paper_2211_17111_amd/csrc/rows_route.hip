@@ -5,20 +5,23 @@
 // above) and holds its logits in registers, V to a lane, so the row is read
 // once, in vectors.  Values are exchanged by rotations within 16 lanes (DPP, at
 // the rate of plain vector instructions).  What bounds the forward is
-// instructions, about a thousand a wave of four rows of 256 logits, so there are
-// two ways to the k largest:
+// instructions: 640 vector, 130 scalar and 23 LDS ones a wave of four rows of 256
+// logits (k = 8, softmax over all experts, counted).  So there are two ways to the k largest:
 //   - k rounds that each find and strike out the largest;
 //   - a list of the few logits that can be among them, ranked pair by pair.
 // Microseconds of the forward, 32,768 rows of float32, weights renormalised,
+// launches back to back in a graph,
 // rounds / list:        k = 2       4          8          12         16
-//   256 experts      8.5 / 8.4  10.7 / 9.2  15.4 / 10.8  19.8 / 16.2  25.0 / 28.4
-//   64 experts       4.7 / 4.8   5.7 / 5.4   7.6 / 5.9    9.6 / 8.0   11.5 / 12.7
-// so 4 to 12 choices take the list (33.5 MB of logits take 7 us).  A butterfly
-// of 64-bit keys through LDS, a wave to a row, took 43 us at 256 experts, k = 8.
+//   256 experts       7.3 / 8.1  9.4 / 8.4  14.3 / 9.9  19.2 / 15.3  24.1 / 26.8
+//   64 experts        4.1 / 4.6  5.1 / 4.7   7.0 / 5.7   8.9 / 7.4   10.8 / 11.7
+// so 4 to 12 choices take the list (33.5 MB of logits take 7 us).  Over all
+// experts instead of renormalised: 11.2 for 9.9.  384 and 512 experts, k = 8, take
+// 31 by rounds of a whole wave.
 //
 // The gradient needs no second softmax: the first chosen expert's weight is
 // exp(0) / sum, so p_e = exp(l_e - l_first) w_first.  The chosen experts' terms
-// go to their places through LDS.  12.5 us for the same rows (67 MB).
+// go to their places through LDS.  13.4 us for the same rows (67 MB), 8.3 where the
+// weights are renormalised and no logit is read.
 
 #include "device_utils.h"
 #include "rows.h"
@@ -44,12 +47,21 @@ __device__ __forceinline__ float value_of(uint32_t o) {
   return __uint_as_float(o ^ (o & 0x80000000u ? 0x80000000u : 0xffffffffu));
 }
 
-// e^d for d <= 0 as the square of 2^(d log2(e) / 2): the hardware's exponential
-// gives no subnormal numbers, the square does.  Two roundings of the exponent
-// and three of the result.
+// e^d for d <= 0.  The hardware's exponential gives no subnormal numbers, so it
+// is taken of half the exponent, h = d log2(e) / 2, and squared.  h is rounded to
+// 24 bits, which alone would be a relative error that grows with |d|: the rest
+// r = d - 2 ln(2) h is what one step of the constant and of h leave, and e^r is
+// 1 + r to far below a rounding.  Measured error of a weight e^d / (1 + e^d):
+// at most 5.7 x 2^-24 for d from -1 to -85 (without r: 18 at -20, 65 at -85).
+// d is held where e^d is 0 already, so that r stays finite; a NaN stays one.
 __device__ __forceinline__ float exp_of(float d) {
-  const float h = __builtin_amdgcn_exp2f(d * 0.72134752f);
-  return h * h;
+  constexpr double k2Ln2 = 1.3862943611198906;
+  constexpr float kHigh = (float)k2Ln2, kLow = (float)(k2Ln2 - (double)kHigh);
+  d = __builtin_elementwise_maximum(d, -256.f);
+  const float h = d * 0.72134752f;
+  const float r = fmaf(h, -kLow, fmaf(h, -kHigh, d));
+  const float p = __builtin_amdgcn_exp2f(h);
+  return p * fmaf(p, r, p);
 }
 
 // The value of the lane ROR lanes on, within 16 lanes.
@@ -275,10 +287,11 @@ __global__ __launch_bounds__(kThreads) void k_route_forward(const T* __restrict_
 #pragma unroll
     for (int i = 0; i < V; ++i) m = fmaxf(m, x[i]);
     m = group_reduce<L>(m, [](float a, float b) { return fmaxf(a, b); });
+    m = m > -INFINITY ? m : 0.f;  // (so that every barred logit lies at -inf from it)
     float sum = 0.f;
     if (!renormalise) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) sum += x[i] > -INFINITY ? exp_of(x[i] - m) : 0.f;
+      for (int i = 0; i < V; ++i) sum += exp_of(x[i] - m);
     }
     uint32_t o[V];
 #pragma unroll
@@ -363,11 +376,12 @@ __global__ __launch_bounds__(kThreads) void k_route_backward(
 #pragma unroll
       for (int i = 0; i < V; ++i) m = fmaxf(m, x[i]);
       m = group_reduce<L>(m, [](float a, float b) { return fmaxf(a, b); });
+      m = m > -INFINITY ? m : 0.f;
       const float w0 = weights[row * k];  // 1 / sum, 0 where no expert could be chosen
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         // (a NaN, or an infinite logit, has made w0 a NaN)
-        const float p = x[i] == -INFINITY ? 0.f * w0 : exp_of(x[i] - m) * w0;
+        const float p = exp_of(x[i] - m) * w0;
         out[i] = p == 0.f ? 0.f : p * (mine[i * L + lane] - s);
       }
     }

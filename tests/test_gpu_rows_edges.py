@@ -117,3 +117,61 @@ def test_combine_keeps_no_operand_that_its_gradients_do_not_read():
         out.backward(g)
         for t, r, v in zip(leaves, on, want):
             assert not r or torch.equal(t.grad, v)
+
+
+# -------------------------------------------------------------------- router
+
+@pytest.mark.parametrize("E,k", [(2, 2), (16, 2), (64, 4), (256, 12), (300, 3)])
+def test_route_weights_of_far_logits(E, k):
+    """A weight's relative error does not grow with its logit's distance.
+
+    Rows of two experts that are not barred, logits 0 and d (their difference is exact).  With the
+    hardware's exponential good to 1 ulp = 2 x 2^-24, e^d is a square (2 x 2 and its rounding 1) whose
+    factor holds the exponent's rounding error to first order (1, and 1 for that and all of second order):
+    7 x 2^-24.  The sum 1 + e^d adds its rounding and e^-5 x 7, the quotient its rounding: 10 x 2^-24.
+    The gradient of g = (0, 1) over all experts, p (1 - w): p is a term (7) times 1 / sum (2.1), rounded
+    (1); 1 - w with w <= e^-5 is off by 1.1, the product by 1: 13 x 2^-24."""
+    T = 4000
+    rng = np.random.default_rng(E)
+    d = -np.exp(rng.uniform(np.log(5), np.log(85), T)).astype(np.float32)  # (p stays a normal number)
+    first = rng.integers(0, E, T)
+    other = (first + 1 + rng.integers(0, E - 1, T)) % E
+    for dtype in (F32, F16):
+        far = torch.from_numpy(d).to(dtype)
+        logits = torch.full((T, E), -float("inf"), dtype=dtype)
+        logits[torch.arange(T), torch.from_numpy(first)] = 0.0
+        logits[torch.arange(T), torch.from_numpy(other)] = far
+        logits = logits.to(DEV)
+        term = np.exp(far.double().numpy())
+        w1 = term / (1 + term)
+        for renormalise in (True, False):
+            weights, ids = rows.route_forward(logits, k, renormalise)
+            want_ids = np.full((T, k), -1, dtype=np.int32)
+            want_ids[:, 0], want_ids[:, 1] = first, other
+            assert np.array_equal(ids.cpu().numpy(), want_ids)
+            _near(weights[:, 1], w1, 10 * U * w1, f"{dtype} renormalise={renormalise}")
+            _near(weights[:, 0], 1 / (1 + term), 3 * U * np.ones(T), "the larger weight")
+            if dtype == F32:
+                g = torch.zeros((T, k), device=DEV)
+                g[:, 1] = 1.0
+                grad = rows.route_backward(g, logits, weights, ids, False)
+                got = grad[torch.arange(T), torch.from_numpy(other)]
+                want = w1 * (1 - w1)
+                _near(got, want, 13 * U * want, f"gradient, renormalise={renormalise}")
+
+
+def test_route_of_the_farthest_logits():
+    """Logits whose difference overflows, and infinite ones, weigh what e^d says."""
+    big, inf = 3.4e38, float("inf")
+    logits = torch.tensor([[big, -big, 0.0], [-big, -big, -big], [0.0, -150.0, -103.0], [-inf, -inf, -inf],
+                           [-inf, -big, -inf], [-big, inf, 0.0]], device=DEV)
+    for renormalise in (True, False):
+        w, ids = rows.route_forward(logits, 2, renormalise)
+        assert ids.tolist() == [[0, 2], [0, 1], [0, 2], [-1, -1], [1, -1], [1, 2]]
+        assert w[0].tolist() == [1.0, 0.0] and w[3].tolist() == [0.0, 0.0] and w[4].tolist() == [1.0, 0.0]
+        share = 0.5 if renormalise else 1 / 3
+        assert (w[1] - share).abs().max() <= 2 * U
+        assert w[2, 0] == 1.0 and abs(float(w[2, 1]) - np.exp(-103.0)) <= 2.0 ** -149  # (its smallest numbers)
+        assert torch.isnan(w[5]).all()
+        grad = rows.route_backward(torch.ones((5, 2), device=DEV), logits[:5], w[:5], ids[:5], renormalise)
+        assert torch.isfinite(grad).all() and not grad[3].any()

@@ -175,3 +175,27 @@ def test_route_of_the_farthest_logits():
         assert torch.isnan(w[5]).all()
         grad = rows.route_backward(torch.ones((5, 2), device=DEV), logits[:5], w[:5], ids[:5], renormalise)
         assert torch.isfinite(grad).all() and not grad[3].any()
+
+
+@pytest.mark.parametrize("renormalise", [True, False])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,E,k", [(37, 8, 8), (35, 16, 12), (50, 16, 4), (33, 20, 4), (19, 32, 12), (18, 33, 9),
+                                   (18, 128, 12), (18, 256, 12), (18, 256, 13), (18, 256, 3)])
+def test_route_on_both_sides_of_the_list(T, E, k, dtype, renormalise):
+    """Every width that 16 lanes take, both ways to the largest, several blocks with a partial last one."""
+    plain.test_route(T, E, k, dtype, renormalise)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,E,k", [(37, 256, 8), (37, 40, 12), (70, 64, 4), (37, 32, 5)])
+def test_route_rows_whose_candidates_overflow_the_list(T, E, k, dtype):
+    """Rows of equal logits (more candidates than are listed, or just as many) among plain ones of a wave."""
+    logits = plain._logits(T, E, dtype, 3)
+    logits[1::4] = 0.5
+    logits[6::8, E // 2:] = 2.0
+    for renormalise in (True, False):
+        w, ids = rows.route_forward(logits, k, renormalise)
+        want_w, want_ids = ref.route_ref(_np(logits), k, renormalise)
+        assert np.array_equal(ids.cpu().numpy(), want_ids)
+        rel = np.take_along_axis(plain._route_rel(_np(logits), E), want_ids, 1)
+        _near(w, want_w, rel * want_w, "weights")

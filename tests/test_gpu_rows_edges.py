@@ -199,3 +199,23 @@ def test_route_rows_whose_candidates_overflow_the_list(T, E, k, dtype):
         assert np.array_equal(ids.cpu().numpy(), want_ids)
         rel = np.take_along_axis(plain._route_rel(_np(logits), E), want_ids, 1)
         _near(w, want_w, rel * want_w, "weights")
+
+
+# ------------------------------------------------------------------ dispatch
+
+@pytest.mark.parametrize("E", [511, 512, 1023, 1024])
+@pytest.mark.parametrize("T,k", [(341, 3), (128, 8), (205, 5), (1024, 1), (100, 7)])
+def test_dispatch_on_both_sides_of_one_launch(T, k, E):
+    """1023, 1024 and 1025 slots, and tables of digits from half full to one key too many."""
+    say(f"dispatch T={T} k={k} E={E}")
+    for C, dtype, kdt, kind in ((24, BF16, torch.int32, "even"), (5, F32, torch.int64, "even"),
+                                (8, F16, torch.int32, "one"), (130, BF16, torch.int64, "low")):
+        ids = _ids(T, k, E, T + E, kind) if kind != "low" else np.random.default_rng(E).integers(-3, 9, (T, k))
+        ids.reshape(-1)[::17] = E  # (dropped like -1, the first key past the table)
+        x = _normal(T, C, dtype=dtype, seed=1)
+        got, plan = rows.dispatch_forward(x, torch.from_numpy(ids).to(kdt).to(DEV), E)
+        want, wplan = ref.dispatch_ref(_np(x), ids, E)
+        _same_plan(plan, wplan, kind)
+        assert np.array_equal(_np(got), want), kind
+        again, _ = rows.dispatch_forward(x, plan)
+        assert torch.equal(again, got)

@@ -219,3 +219,24 @@ def test_dispatch_on_both_sides_of_one_launch(T, k, E):
         assert np.array_equal(_np(got), want), kind
         again, _ = rows.dispatch_forward(x, plan)
         assert torch.equal(again, got)
+
+
+# ------------------------------------------------------------------- sorting
+
+@pytest.mark.parametrize("n", [24, 8192, 8193, 300001])
+@pytest.mark.parametrize("n_keys", [(1 << 30) + 5, (1 << 31) - 2])
+def test_sort_by_keys_of_four_passes(n, n_keys):
+    """The most keys there may be; their offsets (4 and 8 GiB) are compared around every key that occurs."""
+    say(f"sort_keys n={n} n_keys={n_keys}")
+    g = torch.Generator(device=DEV).manual_seed(n)
+    keys = torch.randint(-(1 << 20), (1 << 31) + (1 << 20), (n,), generator=g, device=DEV)
+    keys[:12] = torch.tensor([0, n_keys - 1, n_keys, -1, n_keys + 1, -(1 << 31), (1 << 31) - 1, 1, 1 << 32, 1 << 40,
+                              (1 << 63) - 1, n_keys - 1], device=DEV)
+    keys[n // 2:n // 2 + n // 8] = n_keys // 3  # a frequent one
+    plan = rows.sort_keys(keys, n_keys)
+    ordered, order = torch.sort(torch.where((keys >= 0) & (keys < n_keys), keys, n_keys), stable=True)
+    assert torch.equal(plan.order.long(), order)
+    assert torch.equal(plan.position[order].long(), torch.arange(n, device=DEV))
+    assert plan.offsets.numel() == n_keys + 1
+    near = torch.cat([ordered - 1, ordered, ordered + 1, torch.arange(0, n_keys, 104729, device=DEV)]).clamp(0, n_keys)
+    assert torch.equal(plan.offsets[near].long(), torch.searchsorted(ordered, near))

@@ -240,3 +240,34 @@ def test_sort_by_keys_of_four_passes(n, n_keys):
     assert plan.offsets.numel() == n_keys + 1
     near = torch.cat([ordered - 1, ordered, ordered + 1, torch.arange(0, n_keys, 104729, device=DEV)]).clamp(0, n_keys)
     assert torch.equal(plan.offsets[near].long(), torch.searchsorted(ordered, near))
+
+
+# ------------------------------------------------------------------- streams
+
+def test_values_on_another_stream():
+    """Every call with a stream argument, by value, its inputs ready before."""
+    T, k, E, V = 500, 3, 7, 90
+    x, g = _normal(T, 64), _normal(T, 64, seed=1)
+    ids, tids = torch.from_numpy(_ids(T, k, E, 1)).to(DEV), torch.from_numpy(plain._keys(T, V, 2)).to(DEV)
+    table, logits, w = _normal(V, 64, seed=2), _normal(T, E, seed=3), _normal(T, k, seed=4)
+
+    def calls(**on):
+        r, plan = rows.dispatch_forward(x, ids, E, **on)
+        again, _ = rows.dispatch_forward(x, plan, **on)
+        out = rows.combine_forward(r, w, plan, **on)
+        grads = rows.combine_backward(g, r, w, plan, **on)
+        weights, best = rows.route_forward(logits, k, **on)
+        key = rows.sort_keys(tids, V, **on)
+        e = rows.embed_forward(table, tids, 2.0, **on)
+        return [r, plan.order, plan.position, plan.offsets, again, out, *grads, rows.dispatch_backward(r, plan, k, **on),
+                weights, best, rows.route_backward(w, logits, weights, best, **on), key.order, key.position,
+                key.offsets, e, rows.embed_backward(e, tids, V, 2.0, **on)]
+
+    want = calls()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for s in (side, side.cuda_stream):
+        got = calls(stream=s)
+        side.synchronize()
+        for i, (a, b) in enumerate(zip(got, want)):
+            assert torch.equal(a, b), i

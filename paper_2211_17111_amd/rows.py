@@ -173,13 +173,13 @@ class KeyOrder:
         position, offsets, n_keys = self.position, self.offsets, self.n_keys
         _dense(position, "position", dev, _I32)
         _dense(offsets, "offsets", dev, _I32)
-        if n_keys < 0:  # (the count would lie before the offsets)
-            raise ValueError(f"n_keys = {n_keys} is negative")
-        if position.numel() != n or offsets.numel() != n_keys + 1:
+        if not position.numel() == n < _LIMIT or not offsets.numel() == n_keys + 1 > 0:
+            if n >= _LIMIT:
+                raise ValueError(f"{n} slots exceed 2^31 - 1")
+            if n_keys < 0:  # (the count would lie before the offsets)
+                raise ValueError(f"n_keys = {n_keys} is negative")
             raise ValueError(f"the order has {position.numel()} slots and {offsets.numel()} offsets; "
                              f"{n} slots and {n_keys + 1} offsets are needed")
-        if n >= _LIMIT:
-            raise ValueError(f"{n} slots exceed 2^31 - 1")
         if self.k is not None and self.k != k and n > 0:
             raise ValueError(f"the order has {self.k} slots to a token, not {k}")
         return offsets.data_ptr() + 4 * n_keys
@@ -357,13 +357,13 @@ def combine_backward(grad_out: torch.Tensor, rows: torch.Tensor, weights: torch.
     """(grad_rows, grad_weights) of combine_forward, in the types of rows and
     weights; None for one that is not needed."""
     dev = _device(rows, "rows")
-    _matrix(rows, "rows", dev)
+    stride = _matrix(rows, "rows", dev)
     _dense(weights, "weights", dev, (torch.float32, rows.dtype))
     n, C = rows.shape
     if weights.dim() != 2 or weights.numel() != n:
         raise ValueError(f"weights must be (T, k) for {n} rows, got {tuple(weights.shape)}")
     T, k = weights.shape
-    _matrix(grad_out, "grad_out", dev, shape=(T, C))
+    grad_stride = _matrix(grad_out, "grad_out", dev, shape=(T, C))
     if grad_out.dtype not in (rows.dtype, torch.float32):
         raise ValueError(f"grad_out must be {rows.dtype} or float32, got {grad_out.dtype}")
     kept = plan._check(dev, n, k)
@@ -371,22 +371,27 @@ def combine_backward(grad_out: torch.Tensor, rows: torch.Tensor, weights: torch.
     if ctx is not None:
         with ctx:
             return combine_backward(grad_out, rows, weights, plan, need_rows, need_weights)
-    return _combine_gradients(grad_out, rows if need_weights else None, weights if need_rows else None,
-                              plan.position, kept, (T, k), rows.dtype, weights.dtype)
+    return _combine_gradients(grad_out, grad_stride, rows if need_weights else None, stride,
+                              weights if need_rows else None, plan.position, kept, (T, k, C), rows.dtype,
+                              weights.dtype)
 
 
-def _combine_gradients(grad_out, rows, weights, position, kept: int, shape, rows_dtype, weights_dtype):
+def _combine_gradients(grad_out, grad_stride: int, rows, stride: int, weights, position, kept: int, shape, rows_dtype,
+                       weights_dtype):
     """combine_backward without its checks (kept: the address of the count): the gradient of the rows where the
     weights are given, that of the weights where the rows are (each reads the other operand only)."""
     dev = grad_out.device
-    T, k = shape
-    C = grad_out.shape[1]
-    grad_rows = torch.empty((T * k, C), dtype=rows_dtype, device=dev) if weights is not None else None
-    grad_weights = torch.empty((T, k), dtype=weights_dtype, device=dev) if rows is not None else None
+    T, k, C = shape
+    grad_rows = rows_at = weights_at = grad_rows_at = grad_weights = grad_weights_at = None
+    if weights is not None:
+        grad_rows = torch.empty((T * k, C), dtype=rows_dtype, device=dev)
+        weights_at, grad_rows_at = weights.data_ptr(), grad_rows.data_ptr()
+    if rows is not None:
+        grad_weights = torch.empty((T, k), dtype=weights_dtype, device=dev)
+        rows_at, grad_weights_at = rows.data_ptr(), grad_weights.data_ptr()
     _call("bevpool_combine_backward", T, k, C, _DTYPE_CODE[rows_dtype], _DTYPE_CODE[grad_out.dtype],
-          _DTYPE_CODE[weights_dtype], grad_out.data_ptr(), grad_out.stride(0), _bp._ptr(rows),
-          0 if rows is None else rows.stride(0), _bp._ptr(weights), position.data_ptr(), kept, _bp._ptr(grad_rows),
-          _bp._ptr(grad_weights), _stream(dev))
+          _DTYPE_CODE[weights_dtype], grad_out.data_ptr(), grad_stride, rows_at, stride, weights_at,
+          position.data_ptr(), kept, grad_rows_at, grad_weights_at, _stream(dev))
     return grad_rows, grad_weights
 
 
@@ -492,12 +497,13 @@ class DispatchFunction(torch.autograd.Function):
 class CombineFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, rows, weights, plan, out_dtype):
+        out = combine_forward(rows, weights, plan, out_dtype)
         need_rows, need_weights = ctx.needs_input_grad[:2]
-        ctx.n_keys, ctx.shape, ctx.dtypes = plan.n_keys, weights.shape, (rows.dtype, weights.dtype)
+        ctx.n_keys, ctx.shape, ctx.dtypes = plan.n_keys, (*weights.shape, rows.shape[1]), (rows.dtype, weights.dtype)
         ctx.save_for_backward(rows if need_weights else None, weights if need_rows else None, plan.position,
                               plan.offsets)
         ctx.set_materialize_grads(False)
-        return combine_forward(rows, weights, plan, out_dtype)
+        return out
 
     @staticmethod
     @once_differentiable
@@ -506,9 +512,10 @@ class CombineFunction(torch.autograd.Function):
             return None, None, None, None
         rows, weights, position, offsets = ctx.saved_tensors
         need_rows, need_weights = ctx.needs_input_grad[:2]
-        grads = _combine_gradients(_rows_apart(grad_out), rows if need_weights else None,
-                                   weights if need_rows else None, position, offsets.data_ptr() + 4 * ctx.n_keys,
-                                   ctx.shape, *ctx.dtypes)
+        rows, weights = rows if need_weights else None, weights if need_rows else None
+        grad_out = _rows_apart(grad_out)
+        grads = _combine_gradients(grad_out, grad_out.stride(0), rows, 0 if rows is None else rows.stride(0), weights,
+                                   position, offsets.data_ptr() + 4 * ctx.n_keys, ctx.shape, *ctx.dtypes)
         return *grads, None, None
 
 

@@ -467,7 +467,12 @@ class RouteFunction(torch.autograd.Function):
     def backward(ctx, grad_weights, _):
         if grad_weights is None:
             return None, None, None
-        logits, weights, ids = ctx.saved_tensors
+        logits, weights, ids = ctx.saved_tensors  # (hooks may have replaced them)
+        dev, shape = grad_weights.device, grad_weights.shape
+        _dense(weights, "weights", dev, _F32, shape)
+        _dense(ids, "ids", dev, _I32, shape)
+        if logits is not None:
+            _matrix(logits, "logits", dev, ctx.dtype, (shape[0], ctx.experts))
         return _route_gradient(grad_weights.contiguous(), logits, weights, ids, ctx.experts, ctx.dtype), None, None
 
 
@@ -510,12 +515,17 @@ class CombineFunction(torch.autograd.Function):
     def backward(ctx, grad_out):
         if grad_out is None:
             return None, None, None, None
-        rows, weights, position, offsets = ctx.saved_tensors
+        rows, weights, position, offsets = ctx.saved_tensors  # (hooks may have replaced them)
         need_rows, need_weights = ctx.needs_input_grad[:2]
         rows, weights = rows if need_weights else None, weights if need_rows else None
+        (T, k, C), (rows_dtype, weights_dtype), dev = ctx.shape, ctx.dtypes, grad_out.device
         grad_out = _rows_apart(grad_out)
-        grads = _combine_gradients(grad_out, grad_out.stride(0), rows, 0 if rows is None else rows.stride(0), weights,
-                                   position, offsets.data_ptr() + 4 * ctx.n_keys, ctx.shape, *ctx.dtypes)
+        stride = 0 if rows is None else _matrix(rows, "rows", dev, rows_dtype, (T * k, C))
+        if weights is not None:
+            _dense(weights, "weights", dev, (weights_dtype,), (T, k))
+        kept = KeyOrder(None, position, offsets, ctx.n_keys)._check(dev, T * k, k)
+        grads = _combine_gradients(grad_out, grad_out.stride(0), rows, stride, weights, position, kept, ctx.shape,
+                                   rows_dtype, weights_dtype)
         return *grads, None, None
 
 
@@ -532,7 +542,7 @@ class EmbedFunction(torch.autograd.Function):
     def backward(ctx, grad_out):
         if grad_out is None:
             return None, None, None, None
-        ids, = ctx.saved_tensors
+        ids, = ctx.saved_tensors  # (hooks may have replaced them)
         grad_out = _rows_apart(grad_out) if ids.dim() == 1 else grad_out.contiguous()
         return embed_backward(grad_out, ids, ctx.table_rows, ctx.scale, ctx.dtype), None, None, None
 

@@ -119,6 +119,41 @@ def test_combine_keeps_no_operand_that_its_gradients_do_not_read():
             assert not r or torch.equal(t.grad, v)
 
 
+def _all_forms(x, w_logits, y, w, table, ids, tids, plan, E, k):
+    """Every differentiable form, the router in both."""
+    return [rows.route(w_logits, k)[0], rows.route(w_logits, k, False)[0], rows.dispatch(x, ids, E)[0],
+            rows.dispatch(x, plan)[0], rows.combine(y, w, plan), rows.embed(table, tids, 2.0)]
+
+
+def test_gradients_of_operands_that_hooks_moved_or_changed():
+    """What a gradient keeps may come back through hooks: from the host it is used, in another type or shape refused."""
+    T, k, E, C, V = 11, 3, 6, 20, 15
+    ids, tids = torch.from_numpy(_ids(T, k, E, 1)).to(DEV), torch.from_numpy(plain._keys(T, V, 2)).to(DEV)
+    _, plan = rows.dispatch_forward(_normal(T, C), ids, E)
+    shapes = [(T, C), (T, E), (T * k, C), (T, k), (V, C)]
+    x, l, y, w, table = [_normal(*s, seed=i).requires_grad_() for i, s in enumerate(shapes)]
+
+    def grads():
+        leaves = (x, l, y, w, table)
+        for t in leaves:
+            t.grad = None
+        outs = _all_forms(x, l, y, w, table, ids, tids, plan, E, k)
+        return outs, lambda: (sum((o * o).sum() for o in outs).backward(), [t.grad for t in leaves])[1]
+
+    want = grads()[1]()
+    with torch.autograd.graph.save_on_cpu():
+        _, back = grads()
+        got = back()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    for change in (lambda t: t.half() if t.is_floating_point() else t.short(), lambda t: t[:1] if t.dim() == 2 else t[:4]):
+        with torch.autograd.graph.saved_tensors_hooks(lambda t: t, change):
+            outs, _ = grads()
+        for o in outs:
+            with pytest.raises(ValueError):
+                torch.autograd.backward(o, torch.ones_like(o))
+
+
 # -------------------------------------------------------------------- router
 
 @pytest.mark.parametrize("E,k", [(2, 2), (16, 2), (64, 4), (256, 12), (300, 3)])

@@ -14,8 +14,11 @@
  * Conventions are those of bevpool.h (device pointers owned by the caller,
  * nothing allocated or synchronised, arguments validated before any HIP call,
  * negative bevpool_status, the stream as void*, float32 accumulation rounded
- * once to the output type, every output element written exactly once, no
+ * once to the output type, every output element written with one value, no
  * atomics on floating-point values, bitwise reproducible results), and:
+ *   - a row is moved in vectors of 16 bytes; where its length is not a multiple
+ *     of them, the last one ends with the row and repeats elements of the one
+ *     before, which are then stored twice, with the same value;
  *   - element types are BEVPOOL_F32, BEVPOOL_F16 and BEVPOOL_BF16.  Where a
  *     call has an in_dtype and an out_dtype, they are equal or out_dtype is
  *     F32;

@@ -20,7 +20,8 @@
 // starts of the digits are the offsets; else every key's offset is searched in
 // the sorted keys.
 //
-// Latency is what a call costs: the data of 131,072 slots is 1.5 MB.
+// A call costs its chain of small launches, far from its bytes (1.5 MB for
+// 131,072 slots).
 // Microseconds per sort, launches back to back in a graph, with 128 and with
 // 131,072 keys (two passes and the search):
 //   slots            64   1024   4096   8192  16384  131072  1000000

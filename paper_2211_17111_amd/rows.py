@@ -21,6 +21,15 @@ Matrices may have any distance between their rows (a slice of a wider matrix,
 one row expanded); elements of a row are neighbours.  Everything runs on the
 tensors' device and its current stream, or on ``stream``, which the inputs then
 have to be ready on.  No call synchronises or reads back.
+
+Into a HIP graph the ``*_forward`` and ``*_backward`` calls are captured as they
+are.  A backward pass through the differentiable forms is captured under torch's
+own rule: no graph of the same leaves made outside the capture may be alive, or
+their gradients are added up on a stream that does not take part in it.
+
+A differentiable form keeps for its gradient only what that reads: the router's
+logits where its weights are not renormalised, the rows of a combine where its
+weights need a gradient, the weights where the rows do.
 """
 
 from __future__ import annotations

@@ -8,6 +8,7 @@
  *   route       router: softmax weights of the k best experts of each token
  *   dispatch    token rows in the order of their experts
  *   combine     weighted sum of each token's expert rows
+ *   expert_layer  router weights to output in one call, for a few tokens
  *   embed       lookup of table rows with a scale; its gradient sums the rows
  *               of each id through the sorted order, without atomics
  *
@@ -33,7 +34,8 @@
  *   - outputs must not alias inputs or each other;
  *   - kernels bounds-check every place and id they read;
  *   - limits: n = rows * k < 2^31, n_keys < 2^31 - 1, C <= 2^20,
- *     n_experts <= 1024 and k <= 64 in route.
+ *     n_experts <= 1024 and k <= 64 in route; in expert_layer n_experts <= 1024,
+ *     rows k <= 1024, C and F <= 2^16.
  */
 #ifndef BEVPOOL_ROWS_H
 #define BEVPOOL_ROWS_H
@@ -144,6 +146,27 @@ int bevpool_combine_backward(int64_t rows, int32_t k, int64_t C, int in_dtype, i
                              const void* in, int64_t in_stride, const void* weights,
                              const int32_t* position, const int32_t* kept, void* grad_in,
                              void* grad_weights, void* stream);
+
+/*
+ * Expert layer of a few tokens, without an order: with slot s = t k + j of
+ * expert e = ids[s],
+ *   hidden[s, f] = silu(<x[t], up[e, f]>) <x[t], up[e, F + f]>,  silu(a) = a / (1 + e^-a)
+ *   out[t]       = sum over the kept slots j of t of weights[s] down[e] hidden[s],
+ * up (n_experts x 2F x C) and down (n_experts x C x F) dense, x, up, down and out
+ * of dtype, weights (rows x k) of weight_dtype (F32 or dtype), ids int32 as
+ * bevpool_route_forward writes them (those outside [0, n_experts) are dropped;
+ * experts without a slot are not read).  Sums are float32; hidden is held in
+ * float32, or for a 16-bit dtype in two values of it whose sum has twice its
+ * digits, so that a float16 hidden value past 65504 is infinite.  A token
+ * whose slots are all dropped is zeros.
+ */
+int bevpool_expert_layer_workspace_size(int64_t rows, int32_t k, int64_t C, int64_t F,
+                                        int32_t n_experts, int dtype, size_t* bytes);
+int bevpool_expert_layer_forward(int64_t rows, int32_t k, int64_t C, int64_t F, int32_t n_experts,
+                                 int dtype, int weight_dtype, const void* x, int64_t x_stride,
+                                 const void* up, const void* down, const void* weights,
+                                 const int32_t* ids, void* out, void* workspace,
+                                 size_t workspace_bytes, void* stream);
 
 /*
  * Embedding: out[i] = scale * table[ids[i]], zeros for an id outside

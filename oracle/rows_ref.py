@@ -119,3 +119,32 @@ def embed_backward_ref(grad_out, ids, table_rows: int, scale: float):
     np.add.at(mag, flat[inside], np.abs(scale * g[inside]))
     np.add.at(count, flat[inside], 1)
     return grad, mag, count
+
+
+def expert_layer_ref(x, up, down, weights, ids):
+    """(out, size, slip, reach): the gated layer of every kept slot, and measures
+    of its terms: size the sum of |w down hidden|, slip what out would be off by if
+    gate and value were off by the sums of their terms' magnitudes and the
+    exponential's exponent by 2.5 times itself, reach if hidden were off by 1."""
+    x, up, down, weights = (np.asarray(a, dtype=np.float64) for a in (x, up, down, weights))
+    T, k = weights.shape
+    E, C, F = down.shape
+    out, size, slip, reach = (np.zeros((T, C)) for _ in range(4))
+    for t in range(T):
+        for j in range(k):
+            e = ids[t][j]
+            if not 0 <= e < E:
+                continue
+            gate, value = up[e, :F] @ x[t], up[e, F:] @ x[t]
+            gate_mag, value_mag = np.abs(up[e, :F]) @ np.abs(x[t]), np.abs(up[e, F:]) @ np.abs(x[t])
+            with np.errstate(over="ignore"):
+                s = 1 / (1 + np.exp(-gate))
+            hidden = gate * s * value
+            # (d silu = s (1 + gate (1 - s)), at most 1.1 in size)
+            off = 1.1 * gate_mag * np.abs(value) + np.abs(gate * s) * value_mag + 2.5 * np.abs(gate * hidden)
+            w = np.abs(weights[t, j])
+            out[t] += weights[t, j] * (down[e] @ hidden)
+            size[t] += w * (np.abs(down[e]) @ np.abs(hidden))
+            slip[t] += w * (np.abs(down[e]) @ off)
+            reach[t] += w * np.abs(down[e]).sum(1)
+    return out, size, slip, reach

@@ -1,8 +1,10 @@
 """BEVPoolv2 view-transform path for AMD Instinct MI355X (gfx950).
 
-HIP kernels behind the C ABI of include/bevpool.h and include/bevpool_rows.h,
-with thin ctypes bindings (``paper_2211_17111_amd.bevpool`` for the pooling
-path, ``paper_2211_17111_amd.rows`` for the row operators).
+HIP kernels behind the C ABI of include/bevpool.h, include/bevpool_rows.h and
+include/bevpool_logits.h, with thin ctypes bindings
+(``paper_2211_17111_amd.bevpool`` for the pooling path,
+``paper_2211_17111_amd.rows`` for the row operators,
+``paper_2211_17111_amd.logits`` for the logits operators).
 """
 
 from .bevpool import (  # noqa: F401
@@ -36,6 +38,16 @@ from .bevpool import (  # noqa: F401
     prepare,
     schedule,
 )
+from .logits import (  # noqa: F401
+    Logprobs,
+    distill,
+    distill_backward,
+    distill_forward,
+    distill_step,
+    logprobs,
+    logprobs_backward,
+    logprobs_forward,
+)
 from .rows import (  # noqa: F401
     BEVPOOL_BF16,
     KeyOrder,
@@ -48,6 +60,7 @@ from .rows import (  # noqa: F401
     embed,
     embed_backward,
     embed_forward,
+    expert_layer_forward,
     route,
     route_backward,
     route_forward,

@@ -23,8 +23,8 @@ LIB_PATH = os.path.join(PKG, LIB_NAME)
 
 ARCH = "gfx950"
 SOURCES = ["prepare.hip", "prepare_plan.hip", "schedule_local.hip", "forward.hip", "forward_strips.hip", "forward_dense.hip", "backward.hip", "softmax.hip",
-           "geometry.hip", "rows_sort.hip", "rows_route.hip", "rows_move.hip", "rows_embed.hip",
-           "api.cpp", "rows_api.cpp"]
+           "geometry.hip", "rows_sort.hip", "rows_route.hip", "rows_move.hip", "rows_embed.hip", "rows_layer.hip",
+           "logits_forward.hip", "logits_backward.hip", "api.cpp", "rows_api.cpp", "logits_api.cpp"]
 # measurement probe for bench.py, built into a library of its own
 PROBE_SOURCE = "stream_probe.hip"
 PROBE_LIB = os.path.join(PKG, "libbevpool_probe.so")

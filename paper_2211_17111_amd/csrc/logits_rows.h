@@ -1,0 +1,223 @@
+// Device helpers of the logits operators: teams of threads that share a row,
+// softmax statistics that are joined, and what a row's values are made of.
+//
+// Everything that depends on a row goes through differences from its largest
+// logit m, so that no value is lost to the logits' size: terms e^(scale (x - m))
+// are taken as 2^u, u = (x - m) (scale log2 e), and a log probability is
+// scale (x - m) - log S.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <float.h>
+#include <stdint.h>
+
+#include "device_utils.h"
+#include "logits.h"
+#include "rows_vec.h"
+
+namespace bevpool {
+
+constexpr float kLn2 = 0.693147181f;
+
+// scale log2 e, as one float: its rounding is a relative 2^-25 of the scale.
+inline float exponent_factor(float scale) { return (float)((double)scale * 1.4426950408889634); }
+
+// A team of L threads (a power of two): within a wave up to 64, a workgroup
+// above.  `scratch`: LDS, a float for every wave of a workgroup's team.
+template <int L>
+struct Team {
+  static constexpr int kLanes = L;
+  static constexpr bool kBlock = L > kWave;
+  static constexpr int kWaves = kBlock ? L / kWave : 1;
+  float* scratch;
+
+  __device__ __forceinline__ int lane() const { return threadIdx.x % L; }
+  // Orders the team's accesses to LDS.
+  __device__ __forceinline__ void sync() const {
+    if constexpr (kBlock) {
+      __syncthreads();
+    } else {
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
+  }
+  // f over all threads (f commutes), the same in each.
+  template <class F>
+  __device__ __forceinline__ float reduce(float v, F f) const {
+    constexpr int W = kBlock ? kWave : L;
+#pragma unroll
+    for (int o = W / 2; o > 0; o >>= 1) v = f(v, __shfl_xor(v, o, kWave));
+    if constexpr (kBlock) {
+      if (lane_id() == 0) scratch[threadIdx.x / kWave] = v;
+      lds_barrier();
+      v = scratch[0];
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) v = f(v, scratch[w]);
+      lds_barrier();  // (the scratch may be written again)
+    }
+    return v;
+  }
+  __device__ __forceinline__ float sum(float v) const {
+    return reduce(v, [](float a, float b) { return a + b; });
+  }
+  __device__ __forceinline__ float max(float v) const {
+    return reduce(v, [](float a, float b) { return fmaxf(a, b); });
+  }
+};
+
+// Statistics of some of a row's logits: the largest (r, NaN not counted), the
+// sum s of 2^u with u = c (x - r), and the sum w of u 2^u.  r begins at the
+// lowest number, from which -inf lies at -inf: nothing but -inf leaves s at 0.
+struct Soft {
+  float r, s, w;
+};
+constexpr float kLowest = -FLT_MAX;
+__device__ __forceinline__ Soft no_soft() { return Soft{kLowest, 0.f, 0.f}; }
+
+// u, held where 2^u is 0 anyway, so that u 2^u is 0 there (a NaN stays one).
+__device__ __forceinline__ float held(float u) {
+  return __builtin_elementwise_maximum(u, -256.f);
+}
+
+// The statistics as seen from r (no smaller than a.r).
+__device__ __forceinline__ Soft seen_from(const Soft& a, float r, float c) {
+  const float u = held((a.r - r) * c);
+  const float f = __builtin_amdgcn_exp2f(u);
+  return Soft{r, a.s * f, fmaf(u, a.s, a.w) * f};
+}
+
+// Joins a team's statistics: the same in each thread.
+template <bool ENTROPY, class TEAM>
+__device__ __forceinline__ Soft join(const TEAM& team, Soft a, float c) {
+  a = seen_from(a, team.max(a.r), c);
+  a.s = team.sum(a.s);
+  if constexpr (ENTROPY) a.w = team.sum(a.w);
+  return a;
+}
+
+// Adds N logits (-inf for none).
+template <bool ENTROPY, int N>
+__device__ __forceinline__ void add(Soft& a, const float (&x)[N], float c) {
+  float top = x[0];
+#pragma unroll
+  for (int i = 1; i < N; ++i) top = fmaxf(top, x[i]);
+  if (top > a.r) {
+    if constexpr (ENTROPY) {
+      a = seen_from(a, top, c);
+    } else {
+      a.s *= __builtin_amdgcn_exp2f((a.r - top) * c);
+      a.r = top;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float u = (x[i] - a.r) * c;
+    const float e = __builtin_amdgcn_exp2f(u);
+    a.s += e;
+    if constexpr (ENTROPY) a.w = fmaf(e, held(u), a.w);
+  }
+}
+
+// Logits [0, V) of a row through a team: calls f(x[N], first index) for every
+// vector of this thread, -inf past the end.
+template <typename T, class TEAM, class F>
+__device__ __forceinline__ void for_logits(const TEAM& team, const T* row, int V, F f) {
+  using W = typename RowVec<T>::type;
+  constexpr int N = RowVec<T>::N;
+  const int whole = V / N;
+  for (int i = team.lane(); i < whole; i += TEAM::kLanes) {
+    const W raw = *reinterpret_cast<const W*>(row + i * N);
+    float x[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[e] = (float)raw[e];
+    f(x, i * N);
+  }
+  if (team.lane() == whole % TEAM::kLanes && whole * N < V) {
+    float x[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[e] = whole * N + e < V ? (float)row[whole * N + e] : -INFINITY;
+    f(x, whole * N);
+  }
+}
+
+// A row's distribution from its statistics: S is 0 for a row without one.
+struct Row {
+  float m, S, log_S, scale;
+  __device__ __forceinline__ float logprob(float x) const {
+    return S == 0.f ? -INFINITY : fmaf(scale, x - m, -log_S);
+  }
+};
+__device__ __forceinline__ Row row_of(float m, float S, float scale) {
+  return Row{m, S, S == 0.f ? -INFINITY : logf(S), scale};
+}
+__device__ __forceinline__ Row row_of(const Soft& a, float scale) {
+  return row_of(a.s == 0.f ? -INFINITY : a.r, a.s, scale);
+}
+
+// Id i of an array of int32 or int64 ids, -1 when outside [0, V).
+__device__ __forceinline__ int32_t id_at(const void* ids, int key_type, int64_t i, int32_t V) {
+  const int32_t v = key_type == BEVPOOL_KEY_I32
+                        ? key_or_drop(static_cast<const int32_t*>(ids), i, V)
+                        : key_or_drop(static_cast<const int64_t*>(ids), i, V);
+  return v < V ? v : -1;
+}
+
+// A teacher's side of a row: q_j = e^(t_j - shift), their sum and whether any
+// slot is kept.
+struct Taught {
+  float shift, mass;
+  bool any;
+};
+
+// Slot j of row t: its id, and its log probability (-inf without an id).
+__device__ __forceinline__ int32_t slot_of(const LogitsRows& in, int64_t t, int j, float* logq) {
+  const int32_t id = id_at(in.ids, in.key_type, t * in.k + j, in.V);
+  *logq = id >= 0 ? in.teacher[t * in.k + j] : -INFINITY;
+  return id;
+}
+
+template <class TEAM>
+__device__ __forceinline__ Taught taught(const TEAM& team, const LogitsRows& in, int64_t t) {
+  float top = -INFINITY, sum = 0.f, some = 0.f;
+  for (int j = team.lane(); j < in.k; j += TEAM::kLanes) {
+    float l;
+    slot_of(in, t, j, &l);
+    top = fmaxf(top, l);
+    some = l == -INFINITY ? some : 1.f;  // (a NaN is some)
+  }
+  some = team.max(some);
+  float shift = 0.f;
+  if (in.renormalise) {
+    top = team.max(top);
+    shift = top > -INFINITY ? top : 0.f;
+  }
+  for (int j = team.lane(); j < in.k; j += TEAM::kLanes) {
+    float l;
+    slot_of(in, t, j, &l);
+    sum += expf(l - shift);
+  }
+  sum = team.sum(sum);
+  if (!in.renormalise) return Taught{0.f, sum, some > 0.f};
+  return Taught{shift + logf(sum), 1.f, some > 0.f};
+}
+
+// Divergence of the row's distribution from the teacher's.  (The difference of
+// the log probabilities is taken in 64 bits: a student's that is beyond float32,
+// for a logit of the type's lowest number, may have a small share.)
+template <typename T, class TEAM>
+__device__ __forceinline__ float divergence(const TEAM& team, const LogitsRows& in, int64_t t,
+                                            const T* row, const Row& p, const Taught& q) {
+  float loss = 0.f;
+  for (int j = team.lane(); j < in.k; j += TEAM::kLanes) {
+    float l;
+    const int32_t id = slot_of(in, t, j, &l);
+    if (id < 0 || l == -INFINITY) continue;
+    const float own = expf(l - q.shift);
+    const double behind = (double)p.scale * ((double)p.m - (double)(float)row[id]);
+    if (own != 0.f) loss += p.S == 0.f ? INFINITY : (float)(own * ((l - q.shift) + behind + p.log_S));
+  }
+  return team.sum(loss);
+}
+
+}  // namespace bevpool

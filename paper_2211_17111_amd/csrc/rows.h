@@ -58,6 +58,14 @@ hipError_t launch_combine_backward(int64_t rows, int32_t k, int64_t C, int in_dt
                                    const int32_t* position, const int32_t* kept, void* grad_in,
                                    void* grad_weights, hipStream_t stream);
 
+// Bytes of the hidden values of rows * k slots.
+size_t layer_workspace(int64_t rows, int32_t k, int64_t F, int dtype);
+hipError_t launch_expert_layer(int64_t rows, int32_t k, int64_t C, int64_t F, int32_t n_experts,
+                               int dtype, int weight_dtype, const void* x, int64_t x_stride,
+                               const void* up, const void* down, const void* weights,
+                               const int32_t* ids, void* out, void* workspace,
+                               hipStream_t stream);
+
 hipError_t launch_embed_forward(int64_t n, int64_t table_rows, int64_t C, int in_dtype,
                                 int out_dtype, const void* table, int64_t table_stride,
                                 int key_type, const void* ids, float scale, void* out,

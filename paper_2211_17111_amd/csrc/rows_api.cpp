@@ -5,25 +5,25 @@
 #include <hip/hip_runtime_api.h>
 
 #include "bevpool_rows.h"
+#include "checks.h"
 #include "rows.h"
-#include "status.h"
 
 namespace {
 
+using bevpool::check_dtype;
+using bevpool::check_key_type;
+using bevpool::check_stride;
+using bevpool::check_workspace;
 using bevpool::fail;
 using bevpool::from_hip;
+using bevpool::kIndexLimit;
 using bevpool::ok;
 
-constexpr int64_t kIndexLimit = int64_t(1) << 31;
 constexpr int64_t kMaxC = int64_t(1) << 20;
 constexpr int32_t kMaxExperts = 1024;
 constexpr int32_t kMaxChosen = 64;
-
-int check_dtype(int dtype, const char* what) {
-  if (dtype != BEVPOOL_F32 && dtype != BEVPOOL_F16 && dtype != BEVPOOL_BF16)
-    return fail(BEVPOOL_EDTYPE, "unknown %s %d", what, dtype);
-  return BEVPOOL_OK;
-}
+constexpr int32_t kMaxLayerSlots = 1024;
+constexpr int64_t kMaxLayerColumns = int64_t(1) << 16;
 
 int check_dtypes(int in_dtype, int out_dtype) {
   int st = check_dtype(in_dtype, "in_dtype");
@@ -44,20 +44,9 @@ int check_keys(int64_t n, int64_t n_keys) {
   return BEVPOOL_OK;
 }
 
-int check_key_type(int key_type) {
-  if (key_type != BEVPOOL_KEY_I32 && key_type != BEVPOOL_KEY_I64)
-    return fail(BEVPOOL_EDTYPE, "unknown key type %d", key_type);
-  return BEVPOOL_OK;
-}
-
 int check_columns(int64_t C) {
   if (C < 1) return fail(BEVPOOL_EINVAL, "C = %lld must be >= 1", (long long)C);
   if (C > kMaxC) return fail(BEVPOOL_EOVERFLOW, "C = %lld exceeds %lld", (long long)C, (long long)kMaxC);
-  return BEVPOOL_OK;
-}
-
-int check_stride(int64_t stride, const char* what) {
-  if (stride < 0) return fail(BEVPOOL_EINVAL, "%s = %lld is negative", what, (long long)stride);
   return BEVPOOL_OK;
 }
 
@@ -83,13 +72,6 @@ int check_route(int64_t rows, int32_t n_experts, int32_t k, int dtype, int64_t s
   return st;
 }
 
-int check_workspace(const void* workspace, size_t bytes, size_t need, const char* what) {
-  if (need > 0 && (workspace == nullptr || bytes < need))
-    return fail(BEVPOOL_EWORKSPACE, "%s needs %zu workspace bytes, got %zu at %p", what, need,
-                bytes, workspace);
-  return BEVPOOL_OK;
-}
-
 int check_weight_dtype(int weight_dtype, int in_dtype) {
   int st = check_dtype(weight_dtype, "weight_dtype");
   if (st != BEVPOOL_OK) return st;
@@ -97,6 +79,25 @@ int check_weight_dtype(int weight_dtype, int in_dtype) {
     return fail(BEVPOOL_EDTYPE, "weight_dtype %d is neither in_dtype %d nor float32", weight_dtype,
                 in_dtype);
   return BEVPOOL_OK;
+}
+
+int check_layer(int64_t rows, int32_t k, int64_t C, int64_t F, int32_t n_experts, int dtype) {
+  if (rows < 0) return fail(BEVPOOL_EINVAL, "rows = %lld is negative", (long long)rows);
+  if (k < 1) return fail(BEVPOOL_EINVAL, "k = %d must be >= 1", k);
+  if (rows > kMaxLayerSlots || rows * k > kMaxLayerSlots)
+    return fail(BEVPOOL_EOVERFLOW, "rows * k = %lld * %d exceeds %d", (long long)rows, k,
+                kMaxLayerSlots);
+  for (const int64_t columns : {C, F}) {
+    if (columns < 1)
+      return fail(BEVPOOL_EINVAL, "C = %lld and F = %lld must be >= 1", (long long)C, (long long)F);
+    if (columns > kMaxLayerColumns)
+      return fail(BEVPOOL_EOVERFLOW, "C = %lld or F = %lld exceeds %lld", (long long)C,
+                  (long long)F, (long long)kMaxLayerColumns);
+  }
+  if (n_experts < 1) return fail(BEVPOOL_EINVAL, "n_experts = %d must be >= 1", n_experts);
+  if (n_experts > kMaxExperts)
+    return fail(BEVPOOL_EOVERFLOW, "n_experts = %d exceeds %d", n_experts, kMaxExperts);
+  return check_dtype(dtype, "dtype");
 }
 
 // A launch holds fewer than 2^24 blocks of 256 threads: the kernels of the
@@ -110,12 +111,6 @@ int check_embed_grid(int64_t n, int64_t table_rows, int64_t C) {
                 (long long)C);
   return BEVPOOL_OK;
 }
-
-#define CHECK(call)                        \
-  do {                                     \
-    const int st_ = (call);                \
-    if (st_ != BEVPOOL_OK) return st_;     \
-  } while (0)
 
 }  // namespace
 
@@ -282,6 +277,38 @@ int bevpool_combine_backward(int64_t rows, int32_t k, int64_t C, int in_dtype, i
                                                    position, kept, grad_in, grad_weights,
                                                    static_cast<hipStream_t>(stream)),
                   "bevpool_combine_backward");
+}
+
+int bevpool_expert_layer_workspace_size(int64_t rows, int32_t k, int64_t C, int64_t F,
+                                        int32_t n_experts, int dtype, size_t* bytes) {
+  CHECK(check_layer(rows, k, C, F, n_experts, dtype));
+  REQUIRE_PTR(bytes);
+  *bytes = bevpool::layer_workspace(rows, k, F, dtype);
+  return ok();
+}
+
+int bevpool_expert_layer_forward(int64_t rows, int32_t k, int64_t C, int64_t F, int32_t n_experts,
+                                 int dtype, int weight_dtype, const void* x, int64_t x_stride,
+                                 const void* up, const void* down, const void* weights,
+                                 const int32_t* ids, void* out, void* workspace,
+                                 size_t workspace_bytes, void* stream) {
+  CHECK(check_layer(rows, k, C, F, n_experts, dtype));
+  CHECK(check_weight_dtype(weight_dtype, dtype));
+  CHECK(check_stride(x_stride, "x_stride"));
+  if (rows > 0) {
+    REQUIRE_PTR(x);
+    REQUIRE_PTR(up);
+    REQUIRE_PTR(down);
+    REQUIRE_PTR(weights);
+    REQUIRE_PTR(ids);
+    REQUIRE_PTR(out);
+  }
+  CHECK(check_workspace(workspace, workspace_bytes, bevpool::layer_workspace(rows, k, F, dtype),
+                        "expert_layer_forward"));
+  return from_hip(bevpool::launch_expert_layer(rows, k, C, F, n_experts, dtype, weight_dtype, x,
+                                               x_stride, up, down, weights, ids, out, workspace,
+                                               static_cast<hipStream_t>(stream)),
+                  "bevpool_expert_layer_forward");
 }
 
 int bevpool_embed_forward(int64_t n, int64_t table_rows, int64_t C, int in_dtype, int out_dtype,

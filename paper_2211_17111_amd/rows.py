@@ -1,6 +1,6 @@
 """Row operators of libbevpool.so (include/bevpool_rows.h): router, dispatch
-and combine of expert layers, embedding lookup, and the stable key sort they
-share.
+and combine of expert layers, the whole layer for a few tokens, embedding lookup,
+and the stable key sort they share.
 
 They are the moves of the pooling path for keys that are expert ids or row
 ids: ``sort_keys`` orders slots by key as ``prepare`` orders frustum points by
@@ -16,6 +16,10 @@ forms.  A layer of experts reads
     rows, plan = dispatch(x, ids, n_experts)      # rows of expert e:
     y = experts(rows, plan.offsets)               #   offsets[e] .. offsets[e+1]
     out = combine(y, weights, plan)
+
+and of a few tokens, without gradients, in one call (gated experts, two launches):
+
+    out = expert_layer_forward(x, up, down, *route_forward(logits, k))
 
 Matrices may have any distance between their rows (a slice of a wider matrix,
 one row expanded); elements of a row are neighbours.  Everything runs on the
@@ -63,6 +67,9 @@ _ARGTYPES = {
     "bevpool_combine_forward": [_i64, _i32, _i64, _int, _int, _int, _vp, _i64, _vp, _vp, _vp, _vp, _vp],
     "bevpool_combine_backward": [_i64, _i32, _i64, _int, _int, _int, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp,
                                  _vp],
+    "bevpool_expert_layer_workspace_size": [_i64, _i32, _i64, _i64, _i32, _int, ctypes.POINTER(_sz)],
+    "bevpool_expert_layer_forward": [_i64, _i32, _i64, _i64, _i32, _int, _int, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp,
+                                     _sz, _vp],
     "bevpool_embed_forward": [_i64, _i64, _i64, _int, _int, _vp, _i64, _int, _vp, ctypes.c_float, _vp, _vp],
     "bevpool_embed_backward_workspace_size": [_i64, _i64, _i64, ctypes.POINTER(_sz)],
     "bevpool_embed_backward": [_i64, _i64, _i64, _int, _int, _vp, _i64, _int, _vp, ctypes.c_float, _vp, _vp, _sz,
@@ -402,6 +409,42 @@ def _combine_gradients(grad_out, grad_stride: int, rows, stride: int, weights, p
           _DTYPE_CODE[weights_dtype], grad_out.data_ptr(), grad_stride, rows_at, stride, weights_at,
           position.data_ptr(), kept, grad_rows_at, grad_weights_at, _stream(dev))
     return grad_rows, grad_weights
+
+
+# -------------------------------------------------------------- expert layer
+
+def expert_layer_forward(x: torch.Tensor, up: torch.Tensor, down: torch.Tensor, weights: torch.Tensor,
+                         ids: torch.Tensor, stream=None) -> torch.Tensor:
+    """(T, C): a whole expert layer for a few tokens (T k <= 1024), as decoding calls it,
+    with the router's weights and ids (T, k): the sum over a token's slots of
+    weight * down[e] @ (silu(up[e, :F] @ x) * (up[e, F:] @ x)).  up (E, 2F, C) and
+    down (E, C, F) dense and of x's type; ids int32, those outside [0, E) dropped.
+    It has no gradient: training goes through dispatch and combine."""
+    dev = _device(x, "x")
+    stride = _matrix(x, "x", dev)
+    T, C = x.shape
+    _dense(up, "up", dev, (x.dtype,))
+    _dense(down, "down", dev, (x.dtype,))
+    if down.dim() != 3 or down.shape[1] != C or up.shape != (down.shape[0], 2 * down.shape[2], C):
+        raise ValueError(f"up must be (E, 2F, {C}) and down (E, {C}, F), got {tuple(up.shape)} and {tuple(down.shape)}")
+    E, _, F = down.shape
+    _dense(weights, "weights", dev, (torch.float32, x.dtype))
+    if weights.dim() != 2 or weights.shape[0] != T:
+        raise ValueError(f"weights must be ({T}, k), got {tuple(weights.shape)}")
+    _dense(ids, "ids", dev, _I32, weights.shape)
+    k = weights.shape[1]
+    _check_choices(E, k)
+    ctx = _elsewhere(dev, stream, x, up, down, weights, ids)
+    if ctx is not None:
+        with ctx:
+            return expert_layer_forward(x, up, down, weights, ids)
+    nbytes = _size("bevpool_expert_layer_workspace_size", T, k, C, F, E, _DTYPE_CODE[x.dtype])
+    out = torch.empty((T, C), dtype=x.dtype, device=dev)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    _call("bevpool_expert_layer_forward", T, k, C, F, E, _DTYPE_CODE[x.dtype], _DTYPE_CODE[weights.dtype], x.data_ptr(),
+          stride, up.data_ptr(), down.data_ptr(), weights.data_ptr(), ids.data_ptr(), out.data_ptr(), ws.data_ptr(),
+          nbytes, _stream(dev))
+    return out
 
 
 # ----------------------------------------------------------------- embedding

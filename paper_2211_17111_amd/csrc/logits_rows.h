@@ -96,9 +96,9 @@ __device__ __forceinline__ Soft join(const TEAM& team, Soft a, float c) {
   return a;
 }
 
-// Adds N logits (-inf for none).
+// Adds N logits (-inf for none); the largest of them.
 template <bool ENTROPY, int N>
-__device__ __forceinline__ void add(Soft& a, const float (&x)[N], float c) {
+__device__ __forceinline__ float add(Soft& a, const float (&x)[N], float c) {
   float top = x[0];
 #pragma unroll
   for (int i = 1; i < N; ++i) top = fmaxf(top, x[i]);
@@ -117,28 +117,79 @@ __device__ __forceinline__ void add(Soft& a, const float (&x)[N], float c) {
     a.s += e;
     if constexpr (ENTROPY) a.w = fmaf(e, held(u), a.w);
   }
+  return top;
 }
 
-// Logits [0, V) of a row through a team: calls f(x[N], first index) for every
-// vector of this thread, -inf past the end.
-template <typename T, class TEAM, class F>
-__device__ __forceinline__ void for_logits(const TEAM& team, const T* row, int V, F f) {
+// Vector i of a row of V logits, -inf past its end.
+template <typename T>
+__device__ __forceinline__ typename RowVec<T>::type logits_at(const T* row, int i, int V) {
   using W = typename RowVec<T>::type;
   constexpr int N = RowVec<T>::N;
-  const int whole = V / N;
-  for (int i = team.lane(); i < whole; i += TEAM::kLanes) {
-    const W raw = *reinterpret_cast<const W*>(row + i * N);
-    float x[N];
+  if (i < V / N) return *reinterpret_cast<const W*>(row + i * N);
+  W raw;
 #pragma unroll
-    for (int e = 0; e < N; ++e) x[e] = (float)raw[e];
-    f(x, i * N);
-  }
-  if (team.lane() == whole % TEAM::kLanes && whole * N < V) {
-    float x[N];
+  for (int e = 0; e < N; ++e) raw[e] = i * N + e < V ? row[i * N + e] : (T)-INFINITY;
+  return raw;
+}
+template <typename T>
+inline __host__ __device__ int vectors_of(int64_t V) {
+  return (int)((V + RowVec<T>::N - 1) / RowVec<T>::N);
+}
+
+template <typename T>
+__device__ __forceinline__ void to_floats(const typename RowVec<T>::type& raw, float* x) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) x[e] = whole * N + e < V ? (float)row[whole * N + e] : -INFINITY;
-    f(x, whole * N);
+  for (int e = 0; e < RowVec<T>::N; ++e) x[e] = (float)raw[e];
+}
+
+// A row of at most L NV vectors in the registers of a team: register j of lane l
+// holds vector j L + l.
+template <typename T, int L, int NV>
+struct Held {
+  static constexpr int N = RowVec<T>::N;
+  typename RowVec<T>::type raw[NV];
+
+  __device__ __forceinline__ void load(const T* row, int V, int lane) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) raw[j] = logits_at(row, j * L + lane, V);
   }
+  // f(x[N], vector) for every register, also those past the row's end.
+  template <class F>
+  __device__ __forceinline__ void each(int lane, F f) const {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      float x[N];
+      to_floats<T>(raw[j], x);
+      f(x, j * L + lane);
+    }
+  }
+  // The largest logit of this lane, -inf for none (NaN not counted).
+  __device__ __forceinline__ float largest() const {
+    float m = -INFINITY;
+    each(0, [&](const float (&x)[N], int) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) m = fmaxf(m, x[i]);
+    });
+    return m;
+  }
+};
+
+// The statistics of a held row, the same in each thread; `largest` of this lane.
+template <bool ENTROPY, class TEAM, class H>
+__device__ __forceinline__ Soft soft_of(const TEAM& team, const H& held_row, float largest, float c) {
+  Soft a{fmaxf(team.max(largest), kLowest), 0.f, 0.f};
+  held_row.each(0, [&](const float (&x)[H::N], int) {
+#pragma unroll
+    for (int i = 0; i < H::N; ++i) {
+      const float u = (x[i] - a.r) * c;
+      const float e = __builtin_amdgcn_exp2f(u);
+      a.s += e;
+      if constexpr (ENTROPY) a.w = fmaf(e, held(u), a.w);
+    }
+  });
+  a.s = team.sum(a.s);
+  if constexpr (ENTROPY) a.w = team.sum(a.w);
+  return a;
 }
 
 // A row's distribution from its statistics: S is 0 for a row without one.

@@ -142,29 +142,47 @@ __device__ __forceinline__ void to_floats(const typename RowVec<T>::type& raw, f
   for (int e = 0; e < RowVec<T>::N; ++e) x[e] = (float)raw[e];
 }
 
-// A row of at most L NV vectors in the registers of a team: register j of lane l
-// holds vector j L + l.
+// A row of at most L NV vectors in the registers of a team: vector j L + l in
+// part j of lane l.  Several passes go over it; what one has converted is not to
+// be kept for the next (it would take twice the registers), nor every vector's place, so
+// each part begins with values that the compiler cannot know to be the same.
 template <typename T, int L, int NV>
 struct Held {
   static constexpr int N = RowVec<T>::N;
-  typename RowVec<T>::type raw[NV];
+  typedef int32_t Raw __attribute__((ext_vector_type(4)));
+  Raw raw[NV];
 
   __device__ __forceinline__ void load(const T* row, int V, int lane) {
+    using W = typename RowVec<T>::type;
+    const int whole = V / N;
+    W none;
 #pragma unroll
-    for (int j = 0; j < NV; ++j) raw[j] = logits_at(row, j * L + lane, V);
-  }
-  // f(x[N], vector) for every register, also those past the row's end.
-  template <class F>
-  __device__ __forceinline__ void each(int lane, F f) const {
+    for (int e = 0; e < N; ++e) none[e] = (T)-INFINITY;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
+      raw[j] = __builtin_bit_cast(Raw, none);
+      if (j * L + lane < whole)
+        raw[j] = __builtin_bit_cast(Raw, *reinterpret_cast<const W*>(row + (j * L + lane) * N));
+    }
+    if (whole * N < V) {
+      const Raw last = __builtin_bit_cast(Raw, logits_at(row, whole, V));
+#pragma unroll
+      for (int j = 0; j < NV; ++j) raw[j] = j * L + lane == whole ? last : raw[j];
+    }
+  }
+  // f(x[N], vector) for every part, also those past the row's end.
+  template <class F>
+  __device__ __forceinline__ void each(int lane, F f) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      __asm__ volatile("" : "+v"(raw[j]), "+v"(lane));
       float x[N];
-      to_floats<T>(raw[j], x);
+      to_floats<T>(__builtin_bit_cast(typename RowVec<T>::type, raw[j]), x);
       f(x, j * L + lane);
     }
   }
   // The largest logit of this lane, -inf for none (NaN not counted).
-  __device__ __forceinline__ float largest() const {
+  __device__ __forceinline__ float largest() {
     float m = -INFINITY;
     each(0, [&](const float (&x)[N], int) {
 #pragma unroll
@@ -176,7 +194,7 @@ struct Held {
 
 // The statistics of a held row, the same in each thread; `largest` of this lane.
 template <bool ENTROPY, class TEAM, class H>
-__device__ __forceinline__ Soft soft_of(const TEAM& team, const H& held_row, float largest, float c) {
+__device__ __forceinline__ Soft soft_of(const TEAM& team, H& held_row, float largest, float c) {
   Soft a{fmaxf(team.max(largest), kLowest), 0.f, 0.f};
   held_row.each(0, [&](const float (&x)[H::N], int) {
 #pragma unroll

@@ -70,21 +70,32 @@ __device__ __forceinline__ float kth_largest(float v, int k) {
   return m;
 }
 
-// What a forward writes of a row.
+// What a forward writes of a row.  `Own` is what it needs beside the statistics:
+// loaded ahead of the logits, so that nothing waits for it behind them.
 struct LogprobsRow {
   LogprobsOut out;
-  static constexpr bool kTaught = false;
+  static constexpr bool kEntropy = true;
 
+  struct Own {
+    int32_t id;
+    float x;
+  };
   template <typename T, class TEAM>
-  __device__ __forceinline__ void finish(const TEAM& team, const LogitsRows& in, int64_t t,
-                                         const T* row, const Soft& a, const Row& p) const {
+  __device__ __forceinline__ Own ahead(const TEAM& team, const LogitsRows& in, int64_t t, const T* row) const {
+    Own own{-1, 0.f};
+    if (out.logprob != nullptr && team.lane() == 0) {
+      own.id = id_at(in.ids, in.key_type, t, in.V);
+      if (own.id >= 0) own.x = (float)row[own.id];
+    }
+    return own;
+  }
+  template <class TEAM>
+  __device__ __forceinline__ void finish(const TEAM& team, const LogitsRows&, int64_t t, const Own& own,
+                                         const Soft& a, const Row& p) const {
     if (team.lane() != 0) return;
     out.stats[2 * t] = p.m;
     out.stats[2 * t + 1] = p.S;
-    if (out.logprob != nullptr) {
-      const int32_t id = id_at(in.ids, in.key_type, t, in.V);
-      out.logprob[t] = id >= 0 ? p.logprob((float)row[id]) : 0.f;
-    }
+    if (out.logprob != nullptr) out.logprob[t] = own.id >= 0 ? p.logprob(own.x) : 0.f;
     if (out.lse != nullptr) out.lse[t] = p.S == 0.f ? -INFINITY : fmaf(p.scale, p.m, p.log_S);
     if (out.entropy != nullptr) out.entropy[t] = p.S == 0.f ? 0.f : fmaf(-kLn2, a.w / a.s, p.log_S);
   }
@@ -96,15 +107,26 @@ struct LogprobsRow {
   }
 };
 
+// KS slots to a lane.
+template <int KS>
 struct DistillRow {
   float *loss, *stats;
-  static constexpr bool kTaught = true;
+  static constexpr bool kEntropy = false;
 
+  using Own = Slots<KS>;
   template <typename T, class TEAM>
-  __device__ __forceinline__ void finish(const TEAM& team, const LogitsRows& in, int64_t t,
-                                         const T* row, const Soft&, const Row& p) const {
-    const Taught q = taught(team, in, t);
-    const float d = divergence(team, in, t, row, p, q);
+  __device__ __forceinline__ Own ahead(const TEAM& team, const LogitsRows& in, int64_t t, const T* row) const {
+    Own own;
+    own.load(team, in, t);
+    own.drop();
+    own.load_logits(row);
+    return own;
+  }
+  template <class TEAM>
+  __device__ __forceinline__ void finish(const TEAM& team, const LogitsRows& in, int64_t t, const Own& own,
+                                         const Soft&, const Row& p) const {
+    const Taught q = taught(team, own, in.renormalise);
+    const float d = divergence(team, own, p, q);
     if (team.lane() != 0) return;
     stats[2 * t] = p.m;
     stats[2 * t + 1] = p.S;
@@ -142,12 +164,13 @@ __global__ __launch_bounds__(kThreads) void k_short_rows(LogitsRows in, ROW out,
     const int64_t t = t0 + own;
     if (t >= in.rows) break;  // (a wave's teams need one another nowhere)
     const T* row = static_cast<const T*>(in.logits) + t * in.stride;
+    const auto ahead = out.ahead(team, in, t, row);
     Held<T, L, NV> x;
     x.load(row, in.V, lane);
     const float largest = x.largest();
-    const Soft a = soft_of<!ROW::kTaught>(team, x, largest, c);
+    const Soft a = soft_of<ROW::kEntropy>(team, x, largest, c);
     const Row p = row_of(a, in.scale);
-    out.finish(team, in, t, row, a, p);
+    out.finish(team, in, t, ahead, a, p);
     if constexpr (TOP) {
       const int k = in.k;
       const float from = k <= L ? kth_largest<L>(largest, k) : -INFINITY;
@@ -223,6 +246,8 @@ __global__ __launch_bounds__(kThreads) void k_row_parts(LogitsRows in, ROW out, 
     const int first = (int)(b - t * parts.count) * parts.length;
     const int end = min(first + parts.length, vectors);
     const T* row = static_cast<const T*>(in.logits) + t * in.stride;
+    typename ROW::Own ahead;
+    if (parts.count == 1) ahead = out.ahead(team, in, t, row);
     Soft a = no_soft();
     float largest = -INFINITY;
     int batch = 0;
@@ -255,7 +280,7 @@ __global__ __launch_bounds__(kThreads) void k_row_parts(LogitsRows in, ROW out, 
     a = join<ENTROPY>(team, a, c);
     Row p = row_of(a, in.scale);
     if (parts.count == 1) {
-      out.finish(team, in, t, row, a, p);
+      out.finish(team, in, t, ahead, a, p);
     } else if (tid == 0) {
       parts.soft[b] = Part{a.r, a.s, a.w};
     }
@@ -332,6 +357,7 @@ __global__ __launch_bounds__(kThreads) void k_join_parts(LogitsRows in, ROW out,
   const int tid = threadIdx.x, lane = lane_id(), count = parts.count;
   for (int64_t t = blockIdx.x; t < in.rows; t += gridDim.x) {
     const T* row = static_cast<const T*>(in.logits) + t * in.stride;
+    const auto ahead = out.ahead(team, in, t, row);
     Soft a = no_soft();
     if (tid < count) {
       const Part own = parts.soft[t * count + tid];
@@ -340,7 +366,7 @@ __global__ __launch_bounds__(kThreads) void k_join_parts(LogitsRows in, ROW out,
     if (tid == 0) s_count = 0;
     a = join<ENTROPY>(team, a, c);
     const Row p = row_of(a, in.scale);
-    out.finish(team, in, t, row, a, p);
+    out.finish(team, in, t, ahead, a, p);
     if constexpr (TOP) {
       // The lists are in order: the least of the parts' m-th, m parts >= k, has k
       // pairs no smaller than itself.
@@ -392,27 +418,30 @@ size_t forward_workspace(int64_t rows, int64_t V, int k, int dtype) {
   return rows * cut.count * (sizeof(Part) + k * sizeof(uint64_t)) + 16;  // (16: alignment)
 }
 
-template <typename T, bool ENTROPY, bool TOP, class ROW>
-void launch_rows(const LogitsRows& in, const ROW& out, void* workspace, hipStream_t stream) {
+// Rows that lanes hold; SMALL: what a row has beside its logits fits 16 lanes.
+template <typename T, bool TOP, class SMALL, class ROW>
+void launch_short(const LogitsRows& in, bool small, const SMALL& few_out, const ROW& out, hipStream_t stream) {
   const float c = exponent_factor(in.scale);
   const int vectors = vectors_of<T>(in.V);
-  if (vectors <= kShort) {
-    auto go = [&](auto lanes, auto held) {
-      constexpr int kTeams = kThreads / lanes.value;
-      const int64_t blocks = std::min<int64_t>((in.rows + kTeams - 1) / kTeams, kMaxBlocks);
-      k_short_rows<T, lanes.value, held.value, TOP><<<(unsigned)blocks, kThreads, 0, stream>>>(in, out, c);
-    };
-    constexpr std::integral_constant<int, 16> few;
-    constexpr std::integral_constant<int, kWave> wave;
-    const bool narrow = !TOP || in.k <= 16;
-    if (narrow && vectors <= 16) go(few, std::integral_constant<int, 1>{});
-    else if (narrow && vectors <= 32) go(few, std::integral_constant<int, 2>{});
-    else if (narrow && vectors <= 64) go(few, std::integral_constant<int, 4>{});
-    else if (vectors <= 128) go(wave, std::integral_constant<int, 2>{});
-    else if (vectors <= 256) go(wave, std::integral_constant<int, 4>{});
-    else go(wave, std::integral_constant<int, 8>{});
-    return;
-  }
+  auto go = [&](auto lanes, auto held, const auto& row) {
+    constexpr int kTeams = kThreads / lanes.value;
+    const int64_t blocks = std::min<int64_t>((in.rows + kTeams - 1) / kTeams, kMaxBlocks);
+    k_short_rows<T, lanes.value, held.value, TOP><<<(unsigned)blocks, kThreads, 0, stream>>>(in, row, c);
+  };
+  constexpr std::integral_constant<int, 16> few;
+  constexpr std::integral_constant<int, kWave> wave;
+  if (small && vectors <= 16) go(few, std::integral_constant<int, 1>{}, few_out);
+  else if (small && vectors <= 32) go(few, std::integral_constant<int, 2>{}, few_out);
+  else if (small && vectors <= 64) go(few, std::integral_constant<int, 4>{}, few_out);
+  else if (vectors <= 128) go(wave, std::integral_constant<int, 2>{}, out);
+  else if (vectors <= 256) go(wave, std::integral_constant<int, 4>{}, out);
+  else go(wave, std::integral_constant<int, 8>{}, out);
+}
+
+template <typename T, bool ENTROPY, bool TOP, class ROW>
+void launch_long(const LogitsRows& in, const ROW& out, void* workspace, hipStream_t stream) {
+  const float c = exponent_factor(in.scale);
+  const int vectors = vectors_of<T>(in.V);
   const Cut cut = cut_of(in.rows, vectors, TOP ? in.k : 0);
   Parts parts{in.rows * cut.count, cut.count, cut.length, nullptr, nullptr};
   if (cut.count > 1) {
@@ -442,12 +471,16 @@ hipError_t launch_logprobs_forward(const LogitsRows& in, const LogprobsOut& out,
   by_type(in.dtype, [&](auto t) {
     using T = decltype(t);
     const LogprobsRow row{out};
-    if (out.entropy != nullptr) {
-      if (in.k > 0) launch_rows<T, true, true>(in, row, workspace, stream);
-      else launch_rows<T, true, false>(in, row, workspace, stream);
+    const bool top = in.k > 0, entropy = out.entropy != nullptr;
+    if (vectors_of<T>(in.V) <= kShort) {
+      if (top) launch_short<T, true>(in, in.k <= 16, row, row, stream);
+      else launch_short<T, false>(in, true, row, row, stream);
+    } else if (entropy) {
+      if (top) launch_long<T, true, true>(in, row, workspace, stream);
+      else launch_long<T, true, false>(in, row, workspace, stream);
     } else {
-      if (in.k > 0) launch_rows<T, false, true>(in, row, workspace, stream);
-      else launch_rows<T, false, false>(in, row, workspace, stream);
+      if (top) launch_long<T, false, true>(in, row, workspace, stream);
+      else launch_long<T, false, false>(in, row, workspace, stream);
     }
   });
   return hipGetLastError();
@@ -457,7 +490,11 @@ hipError_t launch_distill_forward(const LogitsRows& in, float* loss, float* stat
                                   hipStream_t stream) {
   if (in.rows == 0) return hipSuccess;
   by_type(in.dtype, [&](auto t) {
-    launch_rows<decltype(t), false, false>(in, DistillRow{loss, stats}, workspace, stream);
+    using T = decltype(t);
+    const DistillRow<1> row{loss, stats};
+    if (vectors_of<T>(in.V) > kShort) launch_long<T, false, false>(in, row, workspace, stream);
+    else if (in.k <= kWave) launch_short<T, false>(in, in.k <= 16, row, row, stream);
+    else launch_short<T, false>(in, false, row, DistillRow<kMaxTaught / kWave>{loss, stats}, stream);
   });
   return hipGetLastError();
 }

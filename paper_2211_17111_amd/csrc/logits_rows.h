@@ -152,23 +152,30 @@ struct Held {
   typedef int32_t Raw __attribute__((ext_vector_type(4)));
   Raw raw[NV];
 
-  __device__ __forceinline__ void load(const T* row, int V, int lane) {
-    using W = typename RowVec<T>::type;
+  __device__ __forceinline__ static Raw none() {
+    typename RowVec<T>::type x;
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[e] = (T)-INFINITY;
+    return __builtin_bit_cast(Raw, x);
+  }
+  __device__ __forceinline__ void load_part(int j, const T* row, int whole, int lane) {
+    raw[j] = none();
+    if (j * L + lane < whole)
+      raw[j] = __builtin_bit_cast(
+          Raw, *reinterpret_cast<const typename RowVec<T>::type*>(row + (j * L + lane) * N));
+  }
+  __device__ __forceinline__ void load_tail(const T* row, int V, int lane) {
     const int whole = V / N;
-    W none;
+    if (whole * N == V) return;
+    const Raw last = __builtin_bit_cast(Raw, logits_at(row, whole, V));
 #pragma unroll
-    for (int e = 0; e < N; ++e) none[e] = (T)-INFINITY;
+    for (int j = 0; j < NV; ++j) raw[j] = j * L + lane == whole ? last : raw[j];
+  }
+
+  __device__ __forceinline__ void load(const T* row, int V, int lane) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      raw[j] = __builtin_bit_cast(Raw, none);
-      if (j * L + lane < whole)
-        raw[j] = __builtin_bit_cast(Raw, *reinterpret_cast<const W*>(row + (j * L + lane) * N));
-    }
-    if (whole * N < V) {
-      const Raw last = __builtin_bit_cast(Raw, logits_at(row, whole, V));
-#pragma unroll
-      for (int j = 0; j < NV; ++j) raw[j] = j * L + lane == whole ? last : raw[j];
-    }
+    for (int j = 0; j < NV; ++j) load_part(j, row, V / N, lane);
+    load_tail(row, V, lane);
   }
   // f(x[N], vector) for every part, also those past the row's end.
   template <class F>
@@ -232,61 +239,86 @@ __device__ __forceinline__ int32_t id_at(const void* ids, int key_type, int64_t 
   return v < V ? v : -1;
 }
 
-// A teacher's side of a row: q_j = e^(t_j - shift), their sum and whether any
+// A row's alternatives by their teacher, slot j in place j / L of lane j % L, and
+// the student's logits for them: -1, -inf and 0 for a slot without an id.
+template <int KS>
+struct Slots {
+  int32_t id[KS];
+  float l[KS];  // log probability
+  float x[KS];
+
+  template <class TEAM>
+  __device__ __forceinline__ void load(const TEAM& team, const LogitsRows& in, int64_t t) {
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      const int j = i * TEAM::kLanes + team.lane();
+      id[i] = j < in.k ? id_at(in.ids, in.key_type, t * in.k + j, in.V) : -1;
+      l[i] = j < in.k ? in.teacher[t * in.k + j] : -INFINITY;
+    }
+  }
+  // (apart from their loading, so that it waits for nothing)
+  __device__ __forceinline__ void drop() {
+#pragma unroll
+    for (int i = 0; i < KS; ++i) l[i] = id[i] >= 0 ? l[i] : -INFINITY;
+  }
+  template <typename T>
+  __device__ __forceinline__ void load_logits(const T* row) {
+#pragma unroll
+    for (int i = 0; i < KS; ++i) x[i] = id[i] >= 0 ? (float)row[id[i]] : 0.f;
+  }
+};
+
+// A teacher's side of a row: q_j = e^(l_j - shift), their sum and whether any
 // slot is kept.
 struct Taught {
   float shift, mass;
   bool any;
 };
 
-// Slot j of row t: its id, and its log probability (-inf without an id).
-__device__ __forceinline__ int32_t slot_of(const LogitsRows& in, int64_t t, int j, float* logq) {
-  const int32_t id = id_at(in.ids, in.key_type, t * in.k + j, in.V);
-  *logq = id >= 0 ? in.teacher[t * in.k + j] : -INFINITY;
-  return id;
-}
-
-template <class TEAM>
-__device__ __forceinline__ Taught taught(const TEAM& team, const LogitsRows& in, int64_t t) {
+template <class TEAM, int KS>
+__device__ __forceinline__ Taught taught(const TEAM& team, const Slots<KS>& slots, bool renormalise) {
   float top = -INFINITY, sum = 0.f, some = 0.f;
-  for (int j = team.lane(); j < in.k; j += TEAM::kLanes) {
-    float l;
-    slot_of(in, t, j, &l);
-    top = fmaxf(top, l);
-    some = l == -INFINITY ? some : 1.f;  // (a NaN is some)
+#pragma unroll
+  for (int i = 0; i < KS; ++i) {
+    top = fmaxf(top, slots.l[i]);
+    some = slots.l[i] == -INFINITY ? some : 1.f;  // (a NaN is some)
   }
   some = team.max(some);
   float shift = 0.f;
-  if (in.renormalise) {
+  if (renormalise) {
     top = team.max(top);
     shift = top > -INFINITY ? top : 0.f;
   }
-  for (int j = team.lane(); j < in.k; j += TEAM::kLanes) {
-    float l;
-    slot_of(in, t, j, &l);
-    sum += expf(l - shift);
-  }
+#pragma unroll
+  for (int i = 0; i < KS; ++i) sum += expf(slots.l[i] - shift);
   sum = team.sum(sum);
-  if (!in.renormalise) return Taught{0.f, sum, some > 0.f};
+  if (!renormalise) return Taught{0.f, sum, some > 0.f};
   return Taught{shift + logf(sum), 1.f, some > 0.f};
 }
 
 // Divergence of the row's distribution from the teacher's.  (The difference of
 // the log probabilities is taken in 64 bits: a student's that is beyond float32,
 // for a logit of the type's lowest number, may have a small share.)
-template <typename T, class TEAM>
-__device__ __forceinline__ float divergence(const TEAM& team, const LogitsRows& in, int64_t t,
-                                            const T* row, const Row& p, const Taught& q) {
+template <class TEAM, int KS>
+__device__ __forceinline__ float divergence(const TEAM& team, const Slots<KS>& slots, const Row& p,
+                                            const Taught& q) {
   float loss = 0.f;
-  for (int j = team.lane(); j < in.k; j += TEAM::kLanes) {
-    float l;
-    const int32_t id = slot_of(in, t, j, &l);
-    if (id < 0 || l == -INFINITY) continue;
-    const float own = expf(l - q.shift);
-    const double behind = (double)p.scale * ((double)p.m - (double)(float)row[id]);
-    if (own != 0.f) loss += p.S == 0.f ? INFINITY : (float)(own * ((l - q.shift) + behind + p.log_S));
+#pragma unroll
+  for (int i = 0; i < KS; ++i) {
+    if (slots.l[i] == -INFINITY) continue;
+    const float own = expf(slots.l[i] - q.shift);
+    const double behind = (double)p.scale * ((double)p.m - (double)slots.x[i]);
+    if (own != 0.f)
+      loss += p.S == 0.f ? INFINITY : (float)(own * ((slots.l[i] - q.shift) + behind + p.log_S));
   }
   return team.sum(loss);
+}
+
+// What a slot adds to its token's gradient, go the row's outgoing one.
+template <int KS>
+__device__ __forceinline__ float slot_gradient(const Slots<KS>& slots, int i, const Taught& q,
+                                               float go, float scale) {
+  return slots.l[i] == -INFINITY ? 0.f : -go * scale * expf(slots.l[i] - q.shift);
 }
 
 }  // namespace bevpool

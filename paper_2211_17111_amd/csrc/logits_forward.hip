@@ -167,7 +167,7 @@ __global__ __launch_bounds__(kThreads) void k_short_rows(LogitsRows in, ROW out,
     const auto ahead = out.ahead(team, in, t, row);
     Held<T, L, NV> x;
     x.load(row, in.V, lane);
-    const float largest = x.largest();
+    const float largest = x.largest(lane);
     const Soft a = soft_of<ROW::kEntropy>(team, x, largest, c);
     const Row p = row_of(a, in.scale);
     out.finish(team, in, t, ahead, a, p);

@@ -143,55 +143,73 @@ __device__ __forceinline__ void to_floats(const typename RowVec<T>::type& raw, f
 }
 
 // A row of at most L NV vectors in the registers of a team: vector j L + l in
-// part j of lane l.  Several passes go over it; what one has converted is not to
-// be kept for the next (it would take twice the registers), nor every vector's place, so
-// each part begins with values that the compiler cannot know to be the same.
+// part j of lane l; what lies behind the row's whole vectors is put in its place,
+// and -inf behind the row's end, where a part is used.  Several passes go over the
+// row; what one has converted is not to be kept for the next (it would take twice
+// the registers), nor every vector's place, so each part begins with values that
+// the compiler cannot know to be the same.
 template <typename T, int L, int NV>
 struct Held {
   static constexpr int N = RowVec<T>::N;
   typedef int32_t Raw __attribute__((ext_vector_type(4)));
-  Raw raw[NV];
+  Raw raw[NV], tail;
+  int whole, vectors;
 
-  __device__ __forceinline__ static Raw none() {
-    typename RowVec<T>::type x;
-#pragma unroll
-    for (int e = 0; e < N; ++e) x[e] = (T)-INFINITY;
-    return __builtin_bit_cast(Raw, x);
+  // Whether part j is asked if it holds logits: each is where several workgroups
+  // share a compute unit (fewer registers, and short rows do nothing for the parts
+  // that they lack), every fourth where one of 1024 threads has it for itself and
+  // needs its parts to overlap.  Loss and gradient of bfloat16 rows, microseconds,
+  // each / every fourth: 8192 of 65,536 (512 threads) 489 and 611, 4096 of 131,072
+  // (1024 threads) 608 and 556.
+  static constexpr bool asked(int j) { return L < 1024 || j % 4 == 0; }
+  // (vectors behind the last whole one load that one; a row must have one)
+  __device__ __forceinline__ void load_part(int j, const T* row, int lane) {
+    raw[j] = __builtin_bit_cast(
+        Raw, *reinterpret_cast<const typename RowVec<T>::type*>(row + min(j * L + lane, whole - 1) * N));
   }
-  __device__ __forceinline__ void load_part(int j, const T* row, int whole, int lane) {
-    raw[j] = none();
-    if (j * L + lane < whole)
-      raw[j] = __builtin_bit_cast(
-          Raw, *reinterpret_cast<const typename RowVec<T>::type*>(row + (j * L + lane) * N));
+  __device__ __forceinline__ void load_tail(const T* row, int V) {
+    tail = __builtin_bit_cast(Raw, logits_at(row, whole, V));
   }
-  __device__ __forceinline__ void load_tail(const T* row, int V, int lane) {
-    const int whole = V / N;
-    if (whole * N == V) return;
-    const Raw last = __builtin_bit_cast(Raw, logits_at(row, whole, V));
-#pragma unroll
-    for (int j = 0; j < NV; ++j) raw[j] = j * L + lane == whole ? last : raw[j];
-  }
-
   __device__ __forceinline__ void load(const T* row, int V, int lane) {
+    whole = V / N;
+    vectors = vectors_of<T>(V);
 #pragma unroll
-    for (int j = 0; j < NV; ++j) load_part(j, row, V / N, lane);
-    load_tail(row, V, lane);
+    for (int j = 0; j < NV; ++j) raw[j] = Raw{};
+    load_tail(row, V);
+    if (whole == 0) return;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      if (asked(j) && j * L >= whole) break;
+      load_part(j, row, lane);
+    }
   }
-  // f(x[N], vector) for every part, also those past the row's end.
+  __device__ __forceinline__ void part(int j, int& lane, float (&x)[N]) {
+    __asm__ volatile("" : "+v"(raw[j]), "+v"(lane));
+    Raw own = raw[j];
+    if ((j + 1) * L > whole) {
+      typename RowVec<T>::type none;
+#pragma unroll
+      for (int e = 0; e < N; ++e) none[e] = (T)-INFINITY;
+      const int i = j * L + lane;
+      own = i < whole ? own : i == whole ? tail : __builtin_bit_cast(Raw, none);
+    }
+    to_floats<T>(__builtin_bit_cast(typename RowVec<T>::type, own), x);
+  }
+  // f(x[N], vector) for every part of the row, also for lanes behind its end.
   template <class F>
   __device__ __forceinline__ void each(int lane, F f) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      __asm__ volatile("" : "+v"(raw[j]), "+v"(lane));
+      if (asked(j) && j * L >= vectors) break;
       float x[N];
-      to_floats<T>(__builtin_bit_cast(typename RowVec<T>::type, raw[j]), x);
+      part(j, lane, x);
       f(x, j * L + lane);
     }
   }
   // The largest logit of this lane, -inf for none (NaN not counted).
-  __device__ __forceinline__ float largest() {
+  __device__ __forceinline__ float largest(int lane) {
     float m = -INFINITY;
-    each(0, [&](const float (&x)[N], int) {
+    each(lane, [&](const float (&x)[N], int) {
 #pragma unroll
       for (int i = 0; i < N; ++i) m = fmaxf(m, x[i]);
     });
@@ -203,7 +221,7 @@ struct Held {
 template <bool ENTROPY, class TEAM, class H>
 __device__ __forceinline__ Soft soft_of(const TEAM& team, H& held_row, float largest, float c) {
   Soft a{fmaxf(team.max(largest), kLowest), 0.f, 0.f};
-  held_row.each(0, [&](const float (&x)[H::N], int) {
+  held_row.each(team.lane(), [&](const float (&x)[H::N], int) {
 #pragma unroll
     for (int i = 0; i < H::N; ++i) {
       const float u = (x[i] - a.r) * c;

@@ -58,8 +58,7 @@ hipError_t launch_combine_backward(int64_t rows, int32_t k, int64_t C, int in_dt
                                    const int32_t* position, const int32_t* kept, void* grad_in,
                                    void* grad_weights, hipStream_t stream);
 
-// Bytes of the hidden values of rows * k slots.
-size_t layer_workspace(int64_t rows, int32_t k, int64_t F, int dtype);
+size_t layer_workspace(int64_t rows, int32_t k, int64_t C, int64_t F, int32_t n_experts, int dtype);
 hipError_t launch_expert_layer(int64_t rows, int32_t k, int64_t C, int64_t F, int32_t n_experts,
                                int dtype, int weight_dtype, const void* x, int64_t x_stride,
                                const void* up, const void* down, const void* weights,

@@ -283,7 +283,7 @@ int bevpool_expert_layer_workspace_size(int64_t rows, int32_t k, int64_t C, int6
                                         int32_t n_experts, int dtype, size_t* bytes) {
   CHECK(check_layer(rows, k, C, F, n_experts, dtype));
   REQUIRE_PTR(bytes);
-  *bytes = bevpool::layer_workspace(rows, k, F, dtype);
+  *bytes = bevpool::layer_workspace(rows, k, C, F, n_experts, dtype);
   return ok();
 }
 
@@ -303,7 +303,8 @@ int bevpool_expert_layer_forward(int64_t rows, int32_t k, int64_t C, int64_t F, 
     REQUIRE_PTR(ids);
     REQUIRE_PTR(out);
   }
-  CHECK(check_workspace(workspace, workspace_bytes, bevpool::layer_workspace(rows, k, F, dtype),
+  CHECK(check_workspace(workspace, workspace_bytes,
+                        bevpool::layer_workspace(rows, k, C, F, n_experts, dtype),
                         "expert_layer_forward"));
   return from_hip(bevpool::launch_expert_layer(rows, k, C, F, n_experts, dtype, weight_dtype, x,
                                                x_stride, up, down, weights, ids, out, workspace,

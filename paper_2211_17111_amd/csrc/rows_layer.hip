@@ -1,5 +1,6 @@
 // Whole expert layer for a few tokens: two launches, the gated products of every
-// slot with its expert's rows, then the weighted sums of their products.
+// slot with its expert's rows, then the weighted sums of their products (and a
+// third that joins these, where few columns are cut into shares).
 //
 // Both are products of an expert's rows with the columns of its few slots, on the
 // matrix cores: 16 rows by 16 slots a tile, rows straight from memory into the
@@ -26,6 +27,9 @@ constexpr int kMaxSlots = 1024;
 constexpr int kUpWaves = 8;
 constexpr int kDownWaves = 16;
 constexpr int kMaxLayerExperts = 1024;
+constexpr int kUnits = 256;           // compute units of the device
+constexpr int kPitch = kTile + 1;     // of a slot's sums in LDS
+constexpr int kSumBytes = kMaxSlots * kPitch * sizeof(float);
 
 typedef float Tile __attribute__((ext_vector_type(4)));
 
@@ -82,7 +86,8 @@ __device__ __forceinline__ void store_hidden(T* at, int64_t low, float v) {
 
 // Workgroup (x, y): hidden values [16 x, 16 x + 16) of the slots of one expert, y
 // itself, or by_slot the expert of slot y if it is the first of its slots.
-template <typename T, int NT>
+// STEPS chunks of a wave are in flight together.
+template <typename T, int NT, int STEPS>
 __global__ __launch_bounds__(kUpWaves * kWave, 4) void k_layer_up(
     const T* __restrict__ x, int64_t x_stride, const T* __restrict__ up,
     const int32_t* __restrict__ ids, int n, Divisor by_k, int C, int F, int E, bool by_slot,
@@ -142,10 +147,11 @@ __global__ __launch_bounds__(kUpWaves * kWave, 4) void k_layer_up(
         }
       }
     };
-    constexpr std::integral_constant<int, 2> several;
+    constexpr std::integral_constant<int, STEPS> several;
     constexpr std::integral_constant<int, 1> single;
     int k0 = wave * K;
-    for (; k0 + kUpWaves * K + K <= C; k0 += 2 * kUpWaves * K) step(std::false_type{}, several, k0);
+    for (; k0 + (STEPS - 1) * kUpWaves * K + K <= C; k0 += STEPS * kUpWaves * K)
+      step(std::false_type{}, several, k0);
     for (; k0 + K <= C; k0 += kUpWaves * K) step(std::false_type{}, single, k0);
     if (k0 < C) step(std::true_type{}, single, k0);
 
@@ -172,27 +178,32 @@ __global__ __launch_bounds__(kUpWaves * kWave, 4) void k_layer_up(
   }
 }
 
-// Workgroup x: outputs [16 x, 16 x + 16) of all tokens.
+// Workgroup (x, y): outputs [16 x, 16 x + 16) of all tokens, from every gridDim.y-th
+// of the items that the experts' products are cut into, a wave to an item: an
+// expert with slots (a group), and one of P parts of its rows' chunks.  Where
+// several workgroups share the items (few columns would leave compute units idle),
+// their sums go to `shares`, which a third launch adds up in their order.  (Adding
+// up by the last of them to arrive took 97 us instead of 17 at one token: its fences
+// write back the caches.)
 template <typename T, typename TW>
 __global__ __launch_bounds__(kDownWaves * kWave) void k_layer_down(
     const T* __restrict__ hidden, const T* __restrict__ down, const TW* __restrict__ weights,
-    const int32_t* __restrict__ ids, int n, int k, Divisor by_k, int C, int F, int E,
-    T* __restrict__ out) {
+    const int32_t* __restrict__ ids, int n, int k, int C, int F, int E, int P,
+    float* __restrict__ shares, T* __restrict__ out) {
   constexpr int kThreads = kDownWaves * kWave;
   constexpr int N = RowVec<T>::N, K = kChunk<T>;
-  constexpr int kPitch = kTile + 1;
   __shared__ int s_count[kMaxLayerExperts];   // slots of an expert, then where they begin
   __shared__ int16_t s_slots[kMaxSlots];      // in the order of their experts
   __shared__ int16_t s_expert[kMaxSlots + 1], s_first[kMaxSlots + 1];  // of every group
   __shared__ int s_scan[kDownWaves];
-  __shared__ float s_part[kDownWaves][kTile * kTile];
-  extern __shared__ float s_sums[];  // n x kPitch: weighted products of every slot
+  extern __shared__ float s_sums[];  // P x n x kPitch: weighted products of every slot
   const int lane = lane_id(), wave = threadIdx.x / kWave;
 
   // The slots by expert.  (The order of an expert's slots is any: each has a
   // column of its own.)
   const int s = threadIdx.x;
   if (s < E) s_count[s] = 0;
+  for (int i = s; i < P * n * kPitch; i += kThreads) s_sums[i] = 0.f;
   lds_barrier();
   int id = s < n ? ids[s] : -1;
   if (id >= E) id = -1;
@@ -216,8 +227,8 @@ __global__ __launch_bounds__(kDownWaves * kWave) void k_layer_down(
 
   const int r = lane % kTile, q = lane / kTile;
   const int c0 = blockIdx.x * kTile;
-  // A tile's sum over the chunks of this wave: first, first + every, ...
-  auto product = [&](int group, int slot0, int chunk0, int every) {
+  // A tile's sum over every P-th chunk from `part` on.
+  auto product = [&](int group, int slot0, int part) {
     const T* row = down + ((int64_t)s_expert[group] * C + min(c0 + r, C - 1)) * F;
     const bool on = slot0 + r < s_first[group + 1];
     const T* high = hidden + (int64_t)s_slots[on ? slot0 + r : slot0] * kPieces<T> * F;
@@ -225,75 +236,94 @@ __global__ __launch_bounds__(kDownWaves * kWave) void k_layer_down(
     auto step = [&](auto check, auto steps, int k0) {
       constexpr bool CHECK = check.value;
       constexpr int S = 2 * steps.value;
-      Part<T> a[S], b[kPieces<T>][S] = {};
+      auto place = [&](int i) { return k0 + i / 2 * P * K + (i % 2 * 4 + q) * N; };
+      Part<T> a[S];
 #pragma unroll
-      for (int i = 0; i < S; ++i)
-        a[i] = part_at<T, CHECK>(row, k0 + i / 2 * every * K + (i % 2 * 4 + q) * N, F);
-      if (on) {
+      for (int i = 0; i < S; ++i) a[i] = part_at<T, CHECK>(row, place(i), F);
 #pragma unroll
-        for (int p = 0; p < kPieces<T>; ++p)
+      for (int i = 0; i < S; ++i) {
+        Part<T> b[kPieces<T>] = {};
+        if (on) {
 #pragma unroll
-          for (int i = 0; i < S; ++i)
-            b[p][i] = part_at<T, CHECK>(high + p * F, k0 + i / 2 * every * K + (i % 2 * 4 + q) * N, F);
+          for (int p = 0; p < kPieces<T>; ++p) b[p] = part_at<T, CHECK>(high + p * F, place(i), F);
+        }
+#pragma unroll
+        for (int p = 0; p < kPieces<T>; ++p) multiply(sum, a[i], b[p]);
       }
-#pragma unroll
-      for (int p = 0; p < kPieces<T>; ++p)
-#pragma unroll
-        for (int i = 0; i < S; ++i) multiply(sum, a[i], b[p][i]);
     };
-    constexpr std::integral_constant<int, 2> several;
+    constexpr std::integral_constant<int, 4> several;
     constexpr std::integral_constant<int, 1> single;
-    int k0 = chunk0 * K;
-    for (; k0 + every * K + K <= F; k0 += 2 * every * K) step(std::false_type{}, several, k0);
-    for (; k0 + K <= F; k0 += every * K) step(std::false_type{}, single, k0);
+    int k0 = part * K;
+    for (; k0 + 3 * P * K + K <= F; k0 += 4 * P * K) step(std::false_type{}, several, k0);
+    for (; k0 + K <= F; k0 += P * K) step(std::false_type{}, single, k0);
     if (k0 < F) step(std::true_type{}, single, k0);
     return sum;
   };
-
-  if (groups >= kDownWaves) {  // a group to a wave
-    for (int g = wave; g < groups; g += kDownWaves)
-      for (int slot0 = s_first[g]; slot0 < s_first[g + 1]; slot0 += kTile) {
-        const Tile sum = product(g, slot0, 0, 1);
-        if (slot0 + r < s_first[g + 1]) {
-          const int slot = s_slots[slot0 + r];
-          const float w = (float)weights[slot];
+  for (int item = blockIdx.y * kDownWaves + wave; item < groups * P; item += gridDim.y * kDownWaves) {
+    const int group = item / P, part = item - group * P;
+    for (int slot0 = s_first[group]; slot0 < s_first[group + 1]; slot0 += kTile) {
+      const Tile sum = product(group, slot0, part);
+      if (slot0 + r < s_first[group + 1]) {
+        const int slot = s_slots[slot0 + r];
+        const float w = (float)weights[slot];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s_sums[slot * kPitch + 4 * q + i] = w * sum[i];
-        }
+        for (int i = 0; i < 4; ++i) s_sums[(part * n + slot) * kPitch + 4 * q + i] = w * sum[i];
       }
-  } else {  // the waves share a group's rows
-    for (int g = 0; g < groups; ++g)
-      for (int slot0 = s_first[g]; slot0 < s_first[g + 1]; slot0 += kTile) {
-        *reinterpret_cast<Tile*>(&s_part[wave][lane * 4]) = product(g, slot0, wave, kDownWaves);
-        __syncthreads();
-        const int i = threadIdx.x;
-        if (i < kTile * kTile && slot0 + i / 4 % kTile < s_first[g + 1]) {
-          const int slot = s_slots[slot0 + i / 4 % kTile];
-          float sum = 0.f;
-#pragma unroll
-          for (int w = 0; w < kDownWaves; ++w) sum += s_part[w][i];
-          s_sums[slot * kPitch + i / 4 / kTile * 4 + i % 4] = (float)weights[slot] * sum;
-        }
-        __syncthreads();
-      }
+    }
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < n / k * kTile; i += kThreads) {
-    const int t = i / kTile, c = i % kTile;
-    if (c0 + c >= C) continue;
+  const int rows = n / k;
+  for (int i = threadIdx.x; i < rows * kTile; i += kThreads) {
+    const int t = i / kTile, c = c0 + i % kTile;
+    if (c >= C) continue;
     float sum = 0.f;
-    for (int j = t * k; j < t * k + k; ++j) {
-      const int e = ids[j];
-      if (e >= 0 && e < E) sum += s_sums[j * kPitch + c];
-    }
-    out[(int64_t)t * C + c0 + c] = (T)sum;
+    for (int j = t * k; j < t * k + k; ++j)
+      for (int p = 0; p < P; ++p) sum += s_sums[(p * n + j) * kPitch + i % kTile];
+    if (gridDim.y > 1) shares[((int64_t)blockIdx.y * rows + t) * C + c] = sum;
+    else out[(int64_t)t * C + c] = (T)sum;
   }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kRowThreads) void k_layer_join(const float* __restrict__ shares,
+                                                            int count, int outputs,
+                                                            T* __restrict__ out) {
+  const int i = blockIdx.x * kRowThreads + threadIdx.x;
+  if (i >= outputs) return;
+  float sum = 0.f;
+#pragma unroll 8
+  for (int y = 0; y < count; ++y) sum += shares[(int64_t)y * outputs + i];
+  out[i] = (T)sum;
+}
+
+// How the second launch is cut, see there; workgroups to a row of them, and parts.
+struct DownCut {
+  int tiles, shares, P;
+};
+DownCut down_cut(int64_t n, int64_t C, int64_t F, int64_t E, int dtype) {
+  const int64_t chunk = dtype == BEVPOOL_F32 ? kChunk<float> : kChunk<half_t>;
+  const int64_t tiles = (C + kTile - 1) / kTile, chunks = (F + chunk - 1) / chunk;
+  const int64_t groups = std::min(n, E);  // (at most)
+  // a workgroup to a compute unit, each wave with a chunk at least
+  const int64_t shares = std::max<int64_t>(
+      1, std::min<int64_t>((kUnits + tiles - 1) / tiles, groups * chunks / kDownWaves));
+  // an item to a wave, as far as the sums of all parts fit LDS
+  const int64_t room = kSumBytes / ((int64_t)sizeof(float) * kPitch * n);
+  const int64_t P = std::max<int64_t>(1, std::min({kDownWaves * shares / groups, chunks, room}));
+  return DownCut{(int)tiles, (int)shares, (int)P};
+}
+
+// Bytes of hidden, behind which the shares lie.
+size_t hidden_bytes(int64_t n, int64_t F) {
+  return (n * F * sizeof(float) + 15) / 16 * 16;  // (two 16-bit pieces take as much)
 }
 
 }  // namespace
 
-size_t layer_workspace(int64_t rows, int32_t k, int64_t F, int dtype) {
-  return (size_t)(rows * k * F) * sizeof(float);  // (two 16-bit pieces take as much)
+size_t layer_workspace(int64_t rows, int32_t k, int64_t C, int64_t F, int32_t n_experts, int dtype) {
+  if (rows == 0) return 0;
+  const DownCut cut = down_cut(rows * k, C, F, n_experts, dtype);
+  return hidden_bytes(rows * k, F) + (cut.shares > 1 ? cut.shares * rows * C * sizeof(float) : 0) + 16;  // (16: alignment)
 }
 
 hipError_t launch_expert_layer(int64_t rows, int32_t k, int64_t C, int64_t F, int32_t n_experts,
@@ -304,25 +334,35 @@ hipError_t launch_expert_layer(int64_t rows, int32_t k, int64_t C, int64_t F, in
   if (rows == 0) return hipSuccess;
   const int n = (int)(rows * k);
   const Divisor by_k = divisor(k);
+  const DownCut cut = down_cut(n, C, F, n_experts, dtype);
+  char* base = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(workspace) + 15) & ~uintptr_t(15));
+  float* shares = reinterpret_cast<float*>(base + hidden_bytes(n, F));
   by_types(dtype, weight_dtype, [&](auto t, auto tw) {
     using T = decltype(t);
     using TW = decltype(tw);
-    T* hidden = static_cast<T*>(workspace);
+    T* hidden = reinterpret_cast<T*>(base);
     const bool by_slot = n <= n_experts;
     const dim3 up_grid((unsigned)((F + kTile - 1) / kTile), (unsigned)(by_slot ? n : n_experts));
-    auto go = [&](auto tiles) {
-      k_layer_up<T, tiles.value><<<up_grid, kUpWaves * kWave, 0, stream>>>(
+    auto go = [&](auto tiles, auto steps) {
+      k_layer_up<T, tiles.value, steps.value><<<up_grid, kUpWaves * kWave, 0, stream>>>(
           static_cast<const T*>(x), x_stride, static_cast<const T*>(up), ids, n, by_k, (int)C,
           (int)F, n_experts, by_slot, hidden);
     };
-    // (an expert's slots: a token chooses it once, as a rule)
-    if (rows <= kTile) go(std::integral_constant<int, 1>{});
-    else if (rows <= 2 * kTile) go(std::integral_constant<int, 2>{});
-    else go(std::integral_constant<int, 4>{});
-    k_layer_down<T, TW><<<(unsigned)((C + kTile - 1) / kTile), kDownWaves * kWave,
-                          n * (kTile + 1) * sizeof(float), stream>>>(
-        hidden, static_cast<const T*>(down), static_cast<const TW*>(weights), ids, n, k, by_k,
-        (int)C, (int)F, n_experts, static_cast<T*>(out));
+    // An expert's slots: a token chooses it once, as a rule, and four times as many
+    // as on the average are rare.  (What does not fit is done in another turn.)
+    const int64_t likely = std::min<int64_t>(rows, 4 * (int64_t)n / n_experts + 1);
+    if (likely <= kTile) go(std::integral_constant<int, 1>{}, std::integral_constant<int, 4>{});
+    else if (likely <= 2 * kTile) go(std::integral_constant<int, 2>{}, std::integral_constant<int, 2>{});
+    else go(std::integral_constant<int, 4>{}, std::integral_constant<int, 2>{});
+    k_layer_down<T, TW><<<dim3(cut.tiles, cut.shares), kDownWaves * kWave,
+                          cut.P * n * kPitch * sizeof(float), stream>>>(
+        hidden, static_cast<const T*>(down), static_cast<const TW*>(weights), ids, n, k, (int)C,
+        (int)F, n_experts, cut.P, shares, static_cast<T*>(out));
+    if (cut.shares > 1) {
+      const int outputs = (int)(rows * C);  // (at most 2^26)
+      k_layer_join<T><<<(outputs + kRowThreads - 1) / kRowThreads, kRowThreads, 0, stream>>>(
+          shares, cut.shares, outputs, static_cast<T*>(out));
+    }
   });
   return hipGetLastError();
 }

@@ -185,7 +185,7 @@ __global__ __launch_bounds__(kUpWaves * kWave, 4) void k_layer_up(
 // their sums go to `shares`, which a third launch adds up in their order.  (Adding
 // up by the last of them to arrive took 97 us instead of 17 at one token: its fences
 // write back the caches.)
-template <typename T, typename TW>
+template <typename T, typename TW, int NT>
 __global__ __launch_bounds__(kDownWaves * kWave) void k_layer_down(
     const T* __restrict__ hidden, const T* __restrict__ down, const TW* __restrict__ weights,
     const int32_t* __restrict__ ids, int n, int k, int C, int F, int E, int P,
@@ -227,47 +227,49 @@ __global__ __launch_bounds__(kDownWaves * kWave) void k_layer_down(
 
   const int r = lane % kTile, q = lane / kTile;
   const int c0 = blockIdx.x * kTile;
-  // A tile's sum over every P-th chunk from `part` on.
-  auto product = [&](int group, int slot0, int part) {
-    const T* row = down + ((int64_t)s_expert[group] * C + min(c0 + r, C - 1)) * F;
-    const bool on = slot0 + r < s_first[group + 1];
-    const T* high = hidden + (int64_t)s_slots[on ? slot0 + r : slot0] * kPieces<T> * F;
-    Tile sum = {};
-    auto step = [&](auto check, auto steps, int k0) {
-      constexpr bool CHECK = check.value;
-      constexpr int S = 2 * steps.value;
-      auto place = [&](int i) { return k0 + i / 2 * P * K + (i % 2 * 4 + q) * N; };
-      Part<T> a[S];
-#pragma unroll
-      for (int i = 0; i < S; ++i) a[i] = part_at<T, CHECK>(row, place(i), F);
-#pragma unroll
-      for (int i = 0; i < S; ++i) {
-        Part<T> b[kPieces<T>] = {};
-        if (on) {
-#pragma unroll
-          for (int p = 0; p < kPieces<T>; ++p) b[p] = part_at<T, CHECK>(high + p * F, place(i), F);
-        }
-#pragma unroll
-        for (int p = 0; p < kPieces<T>; ++p) multiply(sum, a[i], b[p]);
-      }
-    };
-    constexpr std::integral_constant<int, 4> several;
-    constexpr std::integral_constant<int, 1> single;
-    int k0 = part * K;
-    for (; k0 + 3 * P * K + K <= F; k0 += 4 * P * K) step(std::false_type{}, several, k0);
-    for (; k0 + K <= F; k0 += P * K) step(std::false_type{}, single, k0);
-    if (k0 < F) step(std::true_type{}, single, k0);
-    return sum;
-  };
   for (int item = blockIdx.y * kDownWaves + wave; item < groups * P; item += gridDim.y * kDownWaves) {
-    const int group = item / P, part = item - group * P;
-    for (int slot0 = s_first[group]; slot0 < s_first[group + 1]; slot0 += kTile) {
-      const Tile sum = product(group, slot0, part);
-      if (slot0 + r < s_first[group + 1]) {
-        const int slot = s_slots[slot0 + r];
-        const float w = (float)weights[slot];
+    const int group = item / P, part = item - group * P, end = s_first[group + 1];
+    const T* row = down + ((int64_t)s_expert[group] * C + min(c0 + r, C - 1)) * F;
+    for (int first = s_first[group]; first < end; first += NT * kTile) {
+      int slots[NT];  // of this lane, -1 for none
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s_sums[(part * n + slot) * kPitch + 4 * q + i] = w * sum[i];
+      for (int t = 0; t < NT; ++t) slots[t] = first + t * kTile + r < end ? s_slots[first + t * kTile + r] : -1;
+      Tile sum[NT] = {};
+      auto step = [&](auto check, auto steps, int k0) {
+        constexpr bool CHECK = check.value;
+        constexpr int S = 2 * steps.value;
+        auto place = [&](int i) { return k0 + i / 2 * P * K + (i % 2 * 4 + q) * N; };
+        Part<T> a[S];
+#pragma unroll
+        for (int i = 0; i < S; ++i) a[i] = part_at<T, CHECK>(row, place(i), F);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          if (first + t * kTile >= end) break;
+          const T* high = hidden + (int64_t)slots[t] * kPieces<T> * F;
+#pragma unroll
+          for (int i = 0; i < S; ++i) {
+            Part<T> b[kPieces<T>] = {};
+            if (slots[t] >= 0) {
+#pragma unroll
+              for (int p = 0; p < kPieces<T>; ++p) b[p] = part_at<T, CHECK>(high + p * F, place(i), F);
+            }
+#pragma unroll
+            for (int p = 0; p < kPieces<T>; ++p) multiply(sum[t], a[i], b[p]);
+          }
+        }
+      };
+      constexpr std::integral_constant<int, 4> several;
+      constexpr std::integral_constant<int, 1> single;
+      int k0 = part * K;  // every P-th chunk
+      for (; k0 + 3 * P * K + K <= F; k0 += 4 * P * K) step(std::false_type{}, several, k0);
+      for (; k0 + K <= F; k0 += P * K) step(std::false_type{}, single, k0);
+      if (k0 < F) step(std::true_type{}, single, k0);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        if (slots[t] < 0) continue;
+        const float w = (float)weights[slots[t]];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s_sums[(part * n + slots[t]) * kPitch + 4 * q + i] = w * sum[t][i];
       }
     }
   }
@@ -347,6 +349,10 @@ hipError_t launch_expert_layer(int64_t rows, int32_t k, int64_t C, int64_t F, in
       k_layer_up<T, tiles.value, steps.value><<<up_grid, kUpWaves * kWave, 0, stream>>>(
           static_cast<const T*>(x), x_stride, static_cast<const T*>(up), ids, n, by_k, (int)C,
           (int)F, n_experts, by_slot, hidden);
+      k_layer_down<T, TW, tiles.value><<<dim3(cut.tiles, cut.shares), kDownWaves * kWave,
+                                         cut.P * n * kPitch * sizeof(float), stream>>>(
+          hidden, static_cast<const T*>(down), static_cast<const TW*>(weights), ids, n, k, (int)C,
+          (int)F, n_experts, cut.P, shares, static_cast<T*>(out));
     };
     // An expert's slots: a token chooses it once, as a rule, and four times as many
     // as on the average are rare.  (What does not fit is done in another turn.)
@@ -354,10 +360,6 @@ hipError_t launch_expert_layer(int64_t rows, int32_t k, int64_t C, int64_t F, in
     if (likely <= kTile) go(std::integral_constant<int, 1>{}, std::integral_constant<int, 4>{});
     else if (likely <= 2 * kTile) go(std::integral_constant<int, 2>{}, std::integral_constant<int, 2>{});
     else go(std::integral_constant<int, 4>{}, std::integral_constant<int, 2>{});
-    k_layer_down<T, TW><<<dim3(cut.tiles, cut.shares), kDownWaves * kWave,
-                          cut.P * n * kPitch * sizeof(float), stream>>>(
-        hidden, static_cast<const T*>(down), static_cast<const TW*>(weights), ids, n, k, (int)C,
-        (int)F, n_experts, cut.P, shares, static_cast<T*>(out));
     if (cut.shares > 1) {
       const int outputs = (int)(rows * C);  // (at most 2^26)
       k_layer_join<T><<<(outputs + kRowThreads - 1) / kRowThreads, kRowThreads, 0, stream>>>(

@@ -59,15 +59,25 @@ template <int L>
 __device__ __forceinline__ float kth_largest(float v, int k) {
   const int lane = threadIdx.x % L;
   int ahead = 0;
+  if constexpr (L == kWave) {
 #pragma unroll
-  for (int o = 1; o < L; ++o) {
-    const float other = __shfl_xor(v, o, kWave);
-    ahead += other > v || (other == v && (lane ^ o) < lane);
+    for (int i = 0; i < L; ++i) {
+      const float other = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), i));
+      ahead += i < lane ? other >= v : other > v;
+    }
+    const uint64_t mask = wave_ballot(ahead == k - 1);
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), __builtin_ctzll(mask)));
+  } else {
+#pragma unroll
+    for (int o = 1; o < L; ++o) {
+      const float other = __shfl_xor(v, o, kWave);
+      ahead += other > v || (other == v && (lane ^ o) < lane);
+    }
+    float m = ahead == k - 1 ? v : -INFINITY;
+#pragma unroll
+    for (int o = L / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, kWave));
+    return m;
   }
-  float m = ahead == k - 1 ? v : -INFINITY;
-#pragma unroll
-  for (int o = L / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, kWave));
-  return m;
 }
 
 // What a forward writes of a row.  `Own` is what it needs beside the statistics:
@@ -235,7 +245,7 @@ __global__ __launch_bounds__(kThreads) void k_row_parts(LogitsRows in, ROW out, 
     uint64_t list[TOP ? kListed : 1];
   } s;
   __shared__ uint16_t s_batches[kEntries];
-  __shared__ float s_largest[kThreads], s_scratch[kThreads / kWave];
+  __shared__ float s_largest[kThreads], s_scratch[kThreads / kWave], s_from;
   __shared__ uint64_t s_best[kThreads / kWave];
   __shared__ int s_count[2];
   const Team<kThreads> team{s_scratch};
@@ -291,10 +301,15 @@ __global__ __launch_bounds__(kThreads) void k_row_parts(LogitsRows in, ROW out, 
         else parts.pairs[b * k + j] = pair;
       };
       const int lane = lane_id();  // (join's barriers lie behind the maxima)
-      float group = s_largest[lane];
+      if (tid < kWave) {
+        float group = s_largest[lane];
 #pragma unroll
-      for (int w = 1; w < kThreads / kWave; ++w) group = fmaxf(group, s_largest[w * kWave + lane]);
-      const float from = kth_largest<kWave>(group, k);
+        for (int w = 1; w < kThreads / kWave; ++w) group = fmaxf(group, s_largest[w * kWave + lane]);
+        const float kth = kth_largest<kWave>(group, k);
+        if (tid == 0) s_from = kth;
+      }
+      lds_barrier();
+      const float from = s_from;
       for (int i = 0; i < batch; ++i) {
         const float top = s.maxima[i * kThreads + tid];
         if (top >= from && top > -INFINITY) s_batches[atomicAdd(&s_count[0], 1)] = (uint16_t)(i * kThreads + tid);

@@ -150,7 +150,7 @@ template <bool ENTROPY, typename T, class TEAM, class H>
 __device__ __forceinline__ void write_held(const TEAM& team, H& held_row, const T* row, T* out,
                                            const RowGradient& r, int V, float c) {
   const int whole = V / H::N;
-  held_row.each(team.lane(), [&](const float (&x)[H::N], int i) {
+  held_row.each(team.lane(), [&](const float (&x)[H::N], int i, int) {
     float y[H::N] = {};
     if (!r.none) {
 #pragma unroll

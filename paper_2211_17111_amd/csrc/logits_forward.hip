@@ -9,8 +9,8 @@
 //
 // Alternatives: at least k logits are no smaller than the k-th largest of some
 // (disjoint) groups' maxima, so only logits from there on can be chosen: a few
-// more than k, unless many are equal.  The maxima are by-products of the
-// statistics.  The candidates are listed in LDS and each is ranked against the
+// more than k, unless many are equal or the groups are few.  The maxima are
+// by-products of the statistics.  The candidates are listed in LDS and each is ranked against the
 // others; a row with more candidates than the list holds takes k rounds, each of
 // which finds the next in order.
 
@@ -54,30 +54,35 @@ __device__ __forceinline__ uint64_t lanes_max(uint64_t v) {
   return v;
 }
 
-// The k-th largest (k <= L) of the values of L lanes.
-template <int L>
-__device__ __forceinline__ float kth_largest(float v, int k) {
-  const int lane = threadIdx.x % L;
-  int ahead = 0;
-  if constexpr (L == kWave) {
+// A value that at least k of a wave's 64 R values are no smaller than, and as few
+// more as can be: -inf where fewer than k are above it.  (Its order is found bit by
+// bit, the values counted by ballots.)
+template <int R>
+__device__ __forceinline__ float wave_threshold(const uint32_t (&order)[R], int k) {
+  uint32_t from = 0;
+  for (uint32_t bit = 1u << 31; bit != 0; bit >>= 1) {
+    int count = 0;
 #pragma unroll
-    for (int i = 0; i < L; ++i) {
-      const float other = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), i));
-      ahead += i < lane ? other >= v : other > v;
-    }
-    const uint64_t mask = wave_ballot(ahead == k - 1);
-    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), __builtin_ctzll(mask)));
-  } else {
-#pragma unroll
-    for (int o = 1; o < L; ++o) {
-      const float other = __shfl_xor(v, o, kWave);
-      ahead += other > v || (other == v && (lane ^ o) < lane);
-    }
-    float m = ahead == k - 1 ? v : -INFINITY;
-#pragma unroll
-    for (int o = L / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, kWave));
-    return m;
+    for (int r = 0; r < R; ++r) count += __popcll(wave_ballot(order[r] >= (from | bit)));
+    if (count >= k) from |= bit;
+    if (count == k) break;
   }
+  return from > order_of(-FLT_MAX) ? value_of(from) : -INFINITY;
+}
+
+// The same for k <= 16 values of 16 lanes, one each: the k-th largest.
+__device__ __forceinline__ float team_threshold(float v, int k) {
+  const int lane = threadIdx.x % 16;
+  int ahead = 0;
+#pragma unroll
+  for (int o = 1; o < 16; ++o) {
+    const float other = __shfl_xor(v, o, kWave);
+    ahead += other > v || (other == v && (lane ^ o) < lane);
+  }
+  float m = ahead == k - 1 ? v : -INFINITY;
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, kWave));
+  return m;
 }
 
 // What a forward writes of a row.  `Own` is what it needs beside the statistics:
@@ -183,26 +188,58 @@ __global__ __launch_bounds__(kThreads) void k_short_rows(LogitsRows in, ROW out,
     out.finish(team, in, t, ahead, a, p);
     if constexpr (TOP) {
       const int k = in.k;
-      const float from = k <= L ? kth_largest<L>(largest, k) : -INFINITY;
-      if (lane == 0) s_count[own] = 0;
-      team.sync();
-      x.each(lane, [&](const auto& v, int i) {
+      constexpr int N = RowVec<T>::N;
+      int n = 0;
+      if constexpr (L == kWave) {
+        // from the vectors' maxima, or where these may be too few from the logits
+        constexpr bool kSingle = NV == 2;
+        uint32_t order[kSingle ? NV * N : NV] = {};
+        x.each(lane, [&](const auto& v, int, int j) {
+          if constexpr (kSingle) {
 #pragma unroll
-        for (int e = 0; e < RowVec<T>::N; ++e)
-          if (v[e] >= from && v[e] > -INFINITY) {
-            const int at = atomicAdd(&s_count[own], 1);
-            if (at < kListed) s_list[own][at] = pair_of(v[e], i * RowVec<T>::N + e);
+            for (int e = 0; e < N; ++e) order[j * N + e] = order_of(v[e]);
+          } else {
+            float top = v[0];
+#pragma unroll
+            for (int e = 1; e < N; ++e) top = fmaxf(top, v[e]);
+            order[j] = order_of(top);
           }
-      });
-      team.sync();
-      const int n = s_count[own];
+        });
+        const float from = wave_threshold(order, k);
+        x.each(lane, [&](const auto& v, int i, int) {
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            const bool on = v[e] >= from && v[e] > -INFINITY;
+            const uint64_t mask = wave_ballot(on);
+            if (mask == 0) continue;
+            const int at = n + rank_below(mask);
+            if (on && at < kListed) s_list[own][at] = pair_of(v[e], i * N + e);
+            n += __popcll(mask);
+          }
+        });
+        team.sync();
+      } else {
+        const float from = team_threshold(largest, k);
+        if (lane == 0) s_count[own] = 0;
+        team.sync();
+        x.each(lane, [&](const auto& v, int i, int) {
+#pragma unroll
+          for (int e = 0; e < N; ++e)
+            if (v[e] >= from && v[e] > -INFINITY) {
+              const int at = atomicAdd(&s_count[own], 1);
+              if (at < kListed) s_list[own][at] = pair_of(v[e], i * N + e);
+            }
+        });
+        team.sync();
+        n = s_count[own];
+      }
       if (n <= kListed) {
         rank_pairs(team, s_list[own], n, k, [&](int j, uint64_t pair) { out.alternative(t * k + j, pair, p); });
       } else {
         uint64_t last = ~uint64_t(0);
         for (int j = 0; j < k; ++j) {
           uint64_t best = 0;
-          x.each(lane, [&](const auto& v, int i) {
+          x.each(lane, [&](const auto& v, int i, int) {
 #pragma unroll
             for (int e = 0; e < RowVec<T>::N; ++e) {
               const uint64_t pair = pair_of(v[e], i * RowVec<T>::N + e);
@@ -302,11 +339,11 @@ __global__ __launch_bounds__(kThreads) void k_row_parts(LogitsRows in, ROW out, 
       };
       const int lane = lane_id();  // (join's barriers lie behind the maxima)
       if (tid < kWave) {
-        float group = s_largest[lane];
+        uint32_t order[kThreads / kWave];
 #pragma unroll
-        for (int w = 1; w < kThreads / kWave; ++w) group = fmaxf(group, s_largest[w * kWave + lane]);
-        const float kth = kth_largest<kWave>(group, k);
-        if (tid == 0) s_from = kth;
+        for (int w = 0; w < kThreads / kWave; ++w) order[w] = order_of(s_largest[w * kWave + lane]);
+        const float threshold = wave_threshold(order, k);
+        if (tid == 0) s_from = threshold;
       }
       lds_barrier();
       const float from = s_from;
@@ -407,7 +444,10 @@ constexpr int kShort = 512;
 
 // How rows of `vectors` are cut: into parts of whole batches, so that there are
 // about four workgroups to a compute unit, and batches enough for the maxima of a
-// part that alternatives are chosen from.
+// part that alternatives are chosen from.  A part has at least kLeastBatches: of
+// two launches the second costs more than these take (one row of 32,000 bfloat16
+// with 8 alternatives 12.2 us whole, 15.7 in four parts).
+constexpr int kLeastBatches = 4;
 struct Cut {
   int32_t count, length;
 };
@@ -417,7 +457,7 @@ Cut cut_of(int64_t rows, int vectors, int k) {
   int64_t count = rows > 0 ? (1024 + rows - 1) / rows : 1;
   if (k > 0) count = std::max<int64_t>(count, (batches + kMaxBatches - 1) / kMaxBatches);
   count = std::min<int64_t>({count, batches, kMaxParts});
-  const int length = (int)((batches + count - 1) / count);
+  const int length = std::min(batches, std::max(kLeastBatches, (int)((batches + count - 1) / count)));
   return Cut{(batches + length - 1) / length, length * kStep};
 }
 

@@ -195,7 +195,7 @@ struct Held {
     }
     to_floats<T>(__builtin_bit_cast(typename RowVec<T>::type, own), x);
   }
-  // f(x[N], vector) for every part of the row, also for lanes behind its end.
+  // f(x[N], vector, part) for every part of the row, also for lanes behind its end.
   template <class F>
   __device__ __forceinline__ void each(int lane, F f) {
 #pragma unroll
@@ -203,13 +203,13 @@ struct Held {
       if (asked(j) && j * L >= vectors) break;
       float x[N];
       part(j, lane, x);
-      f(x, j * L + lane);
+      f(x, j * L + lane, j);
     }
   }
   // The largest logit of this lane, -inf for none (NaN not counted).
   __device__ __forceinline__ float largest(int lane) {
     float m = -INFINITY;
-    each(lane, [&](const float (&x)[N], int) {
+    each(lane, [&](const float (&x)[N], int, int) {
 #pragma unroll
       for (int i = 0; i < N; ++i) m = fmaxf(m, x[i]);
     });
@@ -221,7 +221,7 @@ struct Held {
 template <bool ENTROPY, class TEAM, class H>
 __device__ __forceinline__ Soft soft_of(const TEAM& team, H& held_row, float largest, float c) {
   Soft a{fmaxf(team.max(largest), kLowest), 0.f, 0.f};
-  held_row.each(team.lane(), [&](const float (&x)[H::N], int) {
+  held_row.each(team.lane(), [&](const float (&x)[H::N], int, int) {
 #pragma unroll
     for (int i = 0; i < H::N; ++i) {
       const float u = (x[i] - a.r) * c;

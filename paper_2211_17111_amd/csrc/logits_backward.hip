@@ -251,7 +251,8 @@ __global__ __launch_bounds__(kThreads) void k_long_gradient(LogitsRows in, G g, 
     // first and 206 from the last)
     const int64_t back = in.rows * parts - 1 - b;
     const int64_t t = parts == 1 ? back : back / parts;
-    const int first = (int)(back - t * parts) * length, end = min(first + length, whole);
+    const int part = (int)(back - t * parts);
+    const int first = part * length, end = min(first + length, whole);
     const T* row = static_cast<const T*>(in.logits) + t * in.stride;
     T* out = grad + t * (int64_t)in.V;
     const RowGradient r = g.of(team, in, t, ids, values);
@@ -277,7 +278,7 @@ __global__ __launch_bounds__(kThreads) void k_long_gradient(LogitsRows in, G g, 
         }
       }
     }
-    const bool last = first + length >= whole;
+    const bool last = part == parts - 1;
     if (last) write_tail<ENTROPY>(team, row, out, r, in.V, c);
     __syncthreads();  // (the marked tokens' values follow the others)
     if (!r.none)

@@ -371,6 +371,46 @@ def test_distill_zero_gradients_and_many_rows():
         assert ((b - wanted)[on].abs() < 1e-6 * g.abs()[on, None].double() + 1e-9).all()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T,V,k", [(1100, 4201, 5), (1500, 9003, 200), (1300, 20001, 64), (1200, 33001, 256), (600, 66000, 17),
+                                   (520, 70003, 100), (513, 131072, 64)])
+def test_distill_step_of_many_long_rows(T, V, k, dtype):
+    """Rows that workgroups take one after the other, with repeated and dropped alternatives: against float64 on the
+    device, under the bounds of this file's head for rows whose logits lie within 40 of their largest, with
+    probabilities of at most 1."""
+    if dtype == F32 and V > 70000:
+        V = 65536 + 3
+    say(f"distill step T={T} V={V} k={k} {dtype}")
+    g = torch.Generator(device=DEV).manual_seed(T)
+    x = (torch.randn((T, V), generator=g, device=DEV) * 2).to(dtype)
+    ids = torch.randint(-V // 20, V + V // 20, (T, k), generator=g, device=DEV)
+    ids[:, 0] = V - 1                       # behind the last whole vector
+    ids[1::2, -1] = ids[1::2, 0]            # twice
+    ids[::7] = -1
+    teacher = torch.log_softmax(torch.randn((T, k), generator=g, device=DEV), 1)
+    go = torch.randn(T, generator=g, device=DEV)
+    go[3::11] = 0
+    loss, grad = lg.distill_step(go, x, ids, teacher, 0.9)
+    inside = (ids >= 0) & (ids < V)
+    some = inside.any(1)
+    q = torch.softmax(torch.where(inside, teacher.double(), -INF), 1)
+    q = torch.where(some[:, None] & inside, q, 0.0)
+    at = torch.where(inside, ids, 0)
+    rel = U * (2.5 * 40 + 4 * CHAIN(V) + 2 * k + 60)
+    half = torch.finfo(dtype).eps / 2
+    for a in range(0, T, 64):
+        b = min(a + 64, T)
+        lp = torch.log_softmax(0.9 * x[a:b].double(), 1)
+        want = torch.where(q[a:b] > 0, q[a:b] * (q[a:b].log() - lp.gather(1, at[a:b])), 0.0).sum(1)
+        assert ((loss[a:b] - want).abs() <= rel * (1 + want.abs())).all()
+        marks = torch.zeros_like(lp).scatter_add_(1, at[a:b], q[a:b])
+        p = lp.exp() * some[a:b, None]
+        wanted = 0.9 * go[a:b, None].double() * (p - marks)
+        bound = 0.9 * go[a:b, None].abs().double() * rel * (p + marks) + wanted.abs() * half + torch.finfo(dtype).smallest_normal
+        assert ((grad[a:b].double() - wanted).abs() <= bound * 1.001).all()
+        assert not grad[a:b][~some[a:b] | (go[a:b] == 0)].any()
+
+
 # ------------------------------------------------------------- shapes, places
 
 def test_strided_and_expanded_rows():
@@ -469,6 +509,33 @@ def test_other_stream():
     s.synchronize()
     for a, b in zip(got, want):
         assert torch.equal(a, b)
+
+
+def test_two_streams_at_once():
+    """Calls of two streams in flight together share nothing."""
+    T, V, k = 3, 200003, 9
+    xs = [_logits(T, V, BF16, i) for i in range(2)]
+    ids = torch.randint(0, V, (T,), device=DEV)
+    tids, teacher = _teacher(T, V, k, 0)
+    tids, g = tids.to(DEV), torch.randn(T, device=DEV)
+
+    def calls(x):
+        r = lg.logprobs_forward(x, ids, k)
+        return [r.logprob, r.top, r.top_ids, *_two_calls(g, x, tids, teacher, 1.0, True)]
+
+    want = [calls(x) for x in xs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in xs]
+    got = [[], []]
+    for _ in range(5):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(calls(xs[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for one in got[i]:
+            for a, b in zip(one, want[i]):
+                assert torch.equal(a, b)
 
 
 def test_graph_replays():

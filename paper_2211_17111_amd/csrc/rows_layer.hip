@@ -84,16 +84,19 @@ __device__ __forceinline__ void store_hidden(T* at, int64_t low, float v) {
     at[low] = __builtin_isinf((float)high) ? (T)0.f : (T)(v - (float)high);
 }
 
-// Workgroup (x, y): hidden values [16 x, 16 x + 16) of the slots of one expert, y
-// itself, or by_slot the expert of slot y if it is the first of its slots.
-// STEPS chunks of a wave are in flight together.
-template <typename T, int NT, int STEPS>
+// Workgroup (x, y): 16 hidden values of the slots of one expert, from 16 x on, y
+// itself, or by_slot the expert of slot y if it is the first of its slots.  HALF: 8
+// values from 8 x on, whose gates and values are the two halves of one tile, where
+// workgroups are few.  STEPS chunks of a wave are in flight together.
+template <typename T, int NT, int STEPS, bool HALF>
 __global__ __launch_bounds__(kUpWaves * kWave, 4) void k_layer_up(
     const T* __restrict__ x, int64_t x_stride, const T* __restrict__ up,
     const int32_t* __restrict__ ids, int n, Divisor by_k, int C, int F, int E, bool by_slot,
     T* __restrict__ hidden) {
+  constexpr int kRows = HALF ? kTile / 2 : kTile;  // hidden values
+  constexpr int kTiles = HALF ? 1 : 2;             // of rows: gates and values
   __shared__ int16_t s_slots[kMaxSlots];
-  __shared__ float s_part[kUpWaves][2][kTile * kTile];
+  __shared__ float s_part[kUpWaves][kTiles][kTile * kTile];
   const int e = by_slot ? ids[blockIdx.y] : (int)blockIdx.y;
   if (e < 0 || e >= E) return;
   const int lane = lane_id(), wave = threadIdx.x / kWave;
@@ -110,9 +113,11 @@ __global__ __launch_bounds__(kUpWaves * kWave, 4) void k_layer_up(
 
   const int r = lane % kTile, q = lane / kTile;
   constexpr int N = RowVec<T>::N, K = kChunk<T>;
-  const int f0 = blockIdx.x * kTile;
-  const T* gate_row = up + ((int64_t)e * 2 * F + min(f0 + r, F - 1)) * C;
-  const T* value_row = gate_row + (int64_t)F * C;
+  const int f0 = blockIdx.x * kRows;
+  const T* row[kTiles];
+#pragma unroll
+  for (int h = 0; h < kTiles; ++h)
+    row[h] = up + ((int64_t)e * 2 * F + (HALF ? r / kRows : h) * F + min(f0 + r % kRows, F - 1)) * C;
   for (int first = 0; first < count; first += NT * kTile) {
     const T* token[NT];
 #pragma unroll
@@ -120,31 +125,28 @@ __global__ __launch_bounds__(kUpWaves * kWave, 4) void k_layer_up(
       const int s = first + t * kTile + r;
       token[t] = s < count ? x + (int64_t)by_k.div(s_slots[s]) * x_stride : nullptr;
     }
-    Tile gate[NT] = {}, value[NT] = {};
+    Tile sum[kTiles][NT] = {};
     auto step = [&](auto check, auto steps, int k0) {
       constexpr bool CHECK = check.value;
       constexpr int S = 2 * steps.value;
-      Part<T> g[S], v[S];
+      auto place = [&](int i) { return k0 + i / 2 * kUpWaves * K + (i % 2 * 4 + q) * N; };
+      Part<T> a[kTiles][S];
 #pragma unroll
-      for (int i = 0; i < S; ++i) {
-        const int at = k0 + i / 2 * kUpWaves * K + (i % 2 * 4 + q) * N;
-        g[i] = part_at<T, CHECK>(gate_row, at, C);
-        v[i] = part_at<T, CHECK>(value_row, at, C);
-      }
+      for (int i = 0; i < S; ++i)
+#pragma unroll
+        for (int h = 0; h < kTiles; ++h) a[h][i] = part_at<T, CHECK>(row[h], place(i), C);
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         if (first + t * kTile >= count) break;
         Part<T> b[S] = {};
         if (token[t] != nullptr) {
 #pragma unroll
-          for (int i = 0; i < S; ++i)
-            b[i] = part_at<T, CHECK>(token[t], k0 + i / 2 * kUpWaves * K + (i % 2 * 4 + q) * N, C);
+          for (int i = 0; i < S; ++i) b[i] = part_at<T, CHECK>(token[t], place(i), C);
         }
 #pragma unroll
-        for (int i = 0; i < S; ++i) {
-          multiply(gate[t], g[i], b[i]);
-          multiply(value[t], v[i], b[i]);
-        }
+        for (int i = 0; i < S; ++i)
+#pragma unroll
+          for (int h = 0; h < kTiles; ++h) multiply(sum[h][t], a[h][i], b[i]);
       }
     };
     constexpr std::integral_constant<int, STEPS> several;
@@ -152,6 +154,10 @@ __global__ __launch_bounds__(kUpWaves * kWave, 4) void k_layer_up(
     int k0 = wave * K;
     for (; k0 + (STEPS - 1) * kUpWaves * K + K <= C; k0 += STEPS * kUpWaves * K)
       step(std::false_type{}, several, k0);
+    if constexpr (STEPS > 2) {
+      constexpr std::integral_constant<int, 2> two;
+      for (; k0 + kUpWaves * K + K <= C; k0 += 2 * kUpWaves * K) step(std::false_type{}, two, k0);
+    }
     for (; k0 + K <= C; k0 += kUpWaves * K) step(std::false_type{}, single, k0);
     if (k0 < C) step(std::true_type{}, single, k0);
 
@@ -159,16 +165,17 @@ __global__ __launch_bounds__(kUpWaves * kWave, 4) void k_layer_up(
     for (int t = 0; t < NT; ++t) {
       if (first + t * kTile >= count) break;
       __syncthreads();  // (what was there has been read)
-      *reinterpret_cast<Tile*>(&s_part[wave][0][lane * 4]) = gate[t];
-      *reinterpret_cast<Tile*>(&s_part[wave][1][lane * 4]) = value[t];
+#pragma unroll
+      for (int h = 0; h < kTiles; ++h) *reinterpret_cast<Tile*>(&s_part[wave][h][lane * 4]) = sum[h][t];
       __syncthreads();
+      // (element 4 l + i of a tile is row 4 (l / 16) + i of slot l % 16)
       const int i = threadIdx.x;
-      if (i < kTile * kTile) {
+      if (i < kRows * kTile) {
         float a = 0.f, b = 0.f;
 #pragma unroll
         for (int w = 0; w < kUpWaves; ++w) {
           a += s_part[w][0][i];
-          b += s_part[w][1][i];
+          b += HALF ? s_part[w][0][i + kRows * kTile] : s_part[w][kTiles - 1][i];
         }
         const int f = f0 + i / 4 / kTile * 4 + i % 4, s = first + t * kTile + i / 4 % kTile;
         if (f < F && s < count)
@@ -259,9 +266,11 @@ __global__ __launch_bounds__(kDownWaves * kWave) void k_layer_down(
         }
       };
       constexpr std::integral_constant<int, 4> several;
+      constexpr std::integral_constant<int, 2> two;
       constexpr std::integral_constant<int, 1> single;
       int k0 = part * K;  // every P-th chunk
       for (; k0 + 3 * P * K + K <= F; k0 += 4 * P * K) step(std::false_type{}, several, k0);
+      for (; k0 + P * K + K <= F; k0 += 2 * P * K) step(std::false_type{}, two, k0);
       for (; k0 + K <= F; k0 += P * K) step(std::false_type{}, single, k0);
       if (k0 < F) step(std::true_type{}, single, k0);
 #pragma unroll
@@ -344,11 +353,26 @@ hipError_t launch_expert_layer(int64_t rows, int32_t k, int64_t C, int64_t F, in
     using TW = decltype(tw);
     T* hidden = reinterpret_cast<T*>(base);
     const bool by_slot = n <= n_experts;
-    const dim3 up_grid((unsigned)((F + kTile - 1) / kTile), (unsigned)(by_slot ? n : n_experts));
-    auto go = [&](auto tiles, auto steps) {
-      k_layer_up<T, tiles.value, steps.value><<<up_grid, kUpWaves * kWave, 0, stream>>>(
-          static_cast<const T*>(x), x_stride, static_cast<const T*>(up), ids, n, by_k, (int)C,
-          (int)F, n_experts, by_slot, hidden);
+    const int columns = by_slot ? n : n_experts;
+    auto up_rows = [&](auto tiles, auto steps, auto half) {
+      constexpr int kRows = half.value ? kTile / 2 : kTile;
+      k_layer_up<T, tiles.value, steps.value, half.value>
+          <<<dim3((unsigned)((F + kRows - 1) / kRows), (unsigned)columns), kUpWaves * kWave, 0, stream>>>(
+              static_cast<const T*>(x), x_stride, static_cast<const T*>(up), ids, n, by_k, (int)C,
+              (int)F, n_experts, by_slot, hidden);
+    };
+    // (few slots on a launch of less than two workgroups to a compute unit: one token
+    // of 6 experts, C 2048, F 1024, 12.7 us and 15.6 with whole tiles)
+    const bool half = (F + kTile - 1) / kTile * std::min(n, n_experts) < 2 * kUnits;
+    constexpr std::integral_constant<int, 2> two;
+    constexpr std::integral_constant<int, 4> four;
+    auto go = [&](auto tiles) {
+      bool done = false;
+      if constexpr (tiles.value == 1) {
+        if (half) up_rows(tiles, four, std::true_type{});
+        done = half;
+      }
+      if (!done) up_rows(tiles, two, std::false_type{});
       k_layer_down<T, TW, tiles.value><<<dim3(cut.tiles, cut.shares), kDownWaves * kWave,
                                          cut.P * n * kPitch * sizeof(float), stream>>>(
           hidden, static_cast<const T*>(down), static_cast<const TW*>(weights), ids, n, k, (int)C,
@@ -357,9 +381,9 @@ hipError_t launch_expert_layer(int64_t rows, int32_t k, int64_t C, int64_t F, in
     // An expert's slots: a token chooses it once, as a rule, and four times as many
     // as on the average are rare.  (What does not fit is done in another turn.)
     const int64_t likely = std::min<int64_t>(rows, 4 * (int64_t)n / n_experts + 1);
-    if (likely <= kTile) go(std::integral_constant<int, 1>{}, std::integral_constant<int, 4>{});
-    else if (likely <= 2 * kTile) go(std::integral_constant<int, 2>{}, std::integral_constant<int, 2>{});
-    else go(std::integral_constant<int, 4>{}, std::integral_constant<int, 2>{});
+    if (likely <= kTile) go(std::integral_constant<int, 1>{});
+    else if (likely <= 2 * kTile) go(two);
+    else go(four);
     if (cut.shares > 1) {
       const int outputs = (int)(rows * C);  // (at most 2^26)
       k_layer_join<T><<<(outputs + kRowThreads - 1) / kRowThreads, kRowThreads, 0, stream>>>(

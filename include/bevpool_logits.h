@@ -25,7 +25,8 @@
  *     dropped ids;
  *   - a row whose outgoing gradients are zero or belong to dropped ids has a
  *     gradient of zeros whatever it holds (padding is not read);
- *   - limits: rows < 2^31, V <= 2^20, k <= 64 in logprobs and <= 256 in distill.
+ *   - limits: rows < 2^31, V <= 2^20, k <= V, and k <= 64 in logprobs, <= 256 in
+ *     distill.
  */
 #ifndef BEVPOOL_LOGITS_H
 #define BEVPOOL_LOGITS_H

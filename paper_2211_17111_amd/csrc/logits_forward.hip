@@ -10,9 +10,15 @@
 // Alternatives: at least k logits are no smaller than the k-th largest of some
 // (disjoint) groups' maxima, so only logits from there on can be chosen: a few
 // more than k, unless many are equal or the groups are few.  The maxima are
-// by-products of the statistics.  The candidates are listed in LDS and each is ranked against the
-// others; a row with more candidates than the list holds takes k rounds, each of
-// which finds the next in order.
+// by-products of the statistics.  The candidates are listed in LDS and each is
+// ranked against the others; a row with more candidates than the list holds takes
+// k rounds, each of which finds the next in order.
+//
+// Measured: 8192 rows of 65,536 bfloat16 183 us, 5.9 TB/s (float32 6.1; at 65,537,
+// where vectors lie across cache lines, 4.8 and 6.1), 190 with the entropy; 4096
+// rows of 131,072 with 20 alternatives 195 us, 5.5 TB/s; 24,000 rows of 118 float32
+// with their divergence 6 us.  (Beginning each row's vectors at a cache line would
+// make a row's sums depend on where it lies.)
 
 #include "logits.h"
 #include "logits_rows.h"

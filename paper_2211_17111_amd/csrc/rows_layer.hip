@@ -7,7 +7,9 @@
 // registers (each is used once), slots' columns out of the caches.  The weights
 // are read once for all slots of an expert, and what bounds the layer is reading
 // them.  A wave takes 128 bytes of each of its 16 rows at a time; the waves of a
-// workgroup take turns along the rows, and their sums are joined in LDS.
+// workgroup take turns along the rows, and their sums are joined in LDS.  64 tokens,
+// 8 of 128 experts, C 4096, F 1280, bfloat16: up 2.6 GB in 480 us (5.5 TB/s), down 1.3
+// GB in 306 (4.3).
 //
 // hidden lies between the launches.  For 16-bit types it is held as two values of
 // the type, hidden = high + low, with a product each: one alone would be a rounding

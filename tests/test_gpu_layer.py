@@ -137,6 +137,15 @@ def test_nan_and_inf_stay_with_their_token():
         assert torch.equal(out[rest], clean[rest])
 
 
+def test_the_same_call_twice_gives_the_same_bits():
+    """However an expert's slots arrive in their list."""
+    for T, k, E in ((64, 8, 12), (512, 2, 3), (3, 4, 8)):
+        args = _inputs(T, k, E, 96, 320, BF16, 7, "any")
+        want = rows.expert_layer_forward(*args)
+        for _ in range(4):
+            assert torch.equal(rows.expert_layer_forward(*args), want)
+
+
 def test_large_gates():
     """silu at both ends: a gate far below zero gives 0, one far above is itself."""
     for dtype in TYPES:

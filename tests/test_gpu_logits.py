@@ -194,6 +194,18 @@ def test_logprobs_long_rows(T, V, k, dtype):
         _check_logprobs(_logits(T, V, dtype, V, kind), ids, k, 1.0, kind, gradients=T * V < 1 << 19)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", [4111, 16391, 50021])
+def test_tokens_at_a_rows_ends(V, dtype):
+    """Given tokens among the elements before a row's first whole cache line and behind its last whole vector, in rows
+    that begin at every place of a line."""
+    T = 13
+    say(f"ends V={V} {dtype}")
+    x = _logits(T, V, dtype, V)
+    for ids in ([0] * T, [V - 1] * T, [(5 * t) % 64 for t in range(T)], [V - 1 - t % 8 for t in range(T)]):
+        _check_logprobs(x, torch.tensor(ids, device=DEV), 2, 1.0, "ends")
+
+
 @pytest.mark.parametrize("k", [1, 2, 16, 17, 40, 63, 64])
 @pytest.mark.parametrize("V", [64, 118, 300, 1000, 5000, 40000])
 def test_alternatives(V, k):

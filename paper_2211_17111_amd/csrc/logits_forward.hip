@@ -553,9 +553,13 @@ hipError_t launch_distill_forward(const LogitsRows& in, float* loss, float* stat
   by_type(in.dtype, [&](auto t) {
     using T = decltype(t);
     const DistillRow<1> row{loss, stats};
+    const DistillRow<4> four{loss, stats};  // (32 slots to 16 lanes, 256 to a wave)
+    static_assert(4 * kWave == kMaxTaught, "slots of a wave");
     if (vectors_of<T>(in.V) > kShort) launch_long<T, false, false>(in, row, workspace, stream);
-    else if (in.k <= kWave) launch_short<T, false>(in, in.k <= 16, row, row, stream);
-    else launch_short<T, false>(in, false, row, DistillRow<kMaxTaught / kWave>{loss, stats}, stream);
+    else if (in.k <= 16) launch_short<T, false>(in, true, row, row, stream);
+    else if (in.k <= 32) launch_short<T, false>(in, true, four, row, stream);
+    else if (in.k <= kWave) launch_short<T, false>(in, false, row, row, stream);
+    else launch_short<T, false>(in, false, four, four, stream);
   });
   return hipGetLastError();
 }

@@ -383,6 +383,17 @@ def test_distill_zero_gradients_and_many_rows():
         assert ((b - wanted)[on].abs() < 1e-6 * g.abs()[on, None].double() + 1e-9).all()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", [64, 118, 255, 300, 511, 2000])
+def test_distill_of_short_rows_with_many_alternatives(V, dtype):
+    for k in (15, 16, 17, 33, 63, 64, 65, 100, 256):
+        if k > V:
+            continue
+        for how in ("plain", "holes", "again"):
+            ids, teacher = _teacher(19, V, k, V + k, how)
+            _check_distill(_logits(19, V, dtype, V), ids.to(DEV), teacher, 1.0, k % 2 == 0, f"{how} k={k}")
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("T,V,k", [(1100, 4201, 5), (1500, 9003, 200), (1300, 20001, 64), (1200, 33001, 256), (600, 66000, 17),
                                    (520, 70003, 100), (513, 131072, 64)])

@@ -155,10 +155,8 @@ int bevpool_combine_backward(int64_t rows, int32_t k, int64_t C, int in_dtype, i
  * up (n_experts x 2F x C) and down (n_experts x C x F) dense, x, up, down and out
  * of dtype, weights (rows x k) of weight_dtype (F32 or dtype), ids int32 as
  * bevpool_route_forward writes them (those outside [0, n_experts) are dropped;
- * experts without a slot are not read).  Sums are float32; hidden is held in
- * float32, or for a 16-bit dtype in two values of it whose sum has twice its
- * digits, so that a float16 hidden value past 65504 is infinite.  A token
- * whose slots are all dropped is zeros.
+ * experts without a slot are not read).  Sums and hidden are float32, whatever
+ * dtype.  A token whose slots are all dropped is zeros.
  */
 int bevpool_expert_layer_workspace_size(int64_t rows, int32_t k, int64_t C, int64_t F,
                                         int32_t n_experts, int dtype, size_t* bytes);

@@ -8,13 +8,14 @@
 // are read once for all slots of an expert, and what bounds the layer is reading
 // them.  A wave takes 128 bytes of each of its 16 rows at a time; the waves of a
 // workgroup take turns along the rows, and their sums are joined in LDS.  64 tokens,
-// 8 of 128 experts, C 4096, F 1280, bfloat16: up 2.6 GB in 480 us (5.5 TB/s), down 1.3
-// GB in 306 (4.3).
+// 8 of 128 experts, C 4096, F 1280, bfloat16: up 2.6 GB in 475 us (5.5 TB/s), down 1.3
+// GB in 320 (4.2).
 //
-// hidden lies between the launches.  For 16-bit types it is held as two values of
-// the type, hidden = high + low, with a product each: one alone would be a rounding
-// as large as the output's own, and both cost 2 F values a slot beside 3 F C a
-// weight matrix.
+// hidden lies between the launches, in float32 whatever the layer's type, and meets
+// down's rows in float32 products: a sum's intermediate has float32's range and digits,
+// and its F values a slot are little beside 3 F C of the weights.  (Two values of the
+// 16-bit type, a product each, took as many bytes and 306 us there, but were infinite
+// past 65504 and lost digits below 2^-3 in float16, and had 16 digits in bfloat16.)
 
 #include "device_utils.h"
 #include "rows.h"
@@ -53,6 +54,27 @@ __device__ __forceinline__ void multiply(Tile& sum, const Part<float>& a, const 
 #pragma unroll
   for (int i = 0; i < 4; ++i) sum = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], sum, 0, 0, 0);
 }
+// The same with slots of float32, whatever the rows' type.
+template <typename T>
+__device__ __forceinline__ void multiply(Tile& sum, const Part<T>& a, const float (&b)[RowVec<T>::N]) {
+#pragma unroll
+  for (int i = 0; i < RowVec<T>::N; ++i)
+    sum = __builtin_amdgcn_mfma_f32_16x16x4f32((float)a[i], b[i], sum, 0, 0, 0);
+}
+// The same of the first 4 FEW of 16 slots, in a quarter of the time for every four:
+// 16 products of four slots by four rows, one for each quarter of 16 lanes, which is
+// given the slots of lanes 4 u .. + 3 of these (the broadcast 2, u).  Lane l's results
+// are row l % 16 of slots 4 u .. + 3, over the elements that its 16 lanes hold.  (A
+// tile of 16 slots, with four in it on the average: the layer above 835 us, by fours 801.)
+template <typename T, int FEW>
+__device__ __forceinline__ void multiply_few(Tile (&sum)[FEW], const Part<T>& a, const float (&b)[RowVec<T>::N]) {
+  static_assert(FEW <= 2, "broadcasts");
+#pragma unroll
+  for (int i = 0; i < RowVec<T>::N; ++i) {
+    sum[0] = __builtin_amdgcn_mfma_f32_4x4x1f32(b[i], (float)a[i], sum[0], 2, 0, 0);
+    if constexpr (FEW > 1) sum[1] = __builtin_amdgcn_mfma_f32_4x4x1f32(b[i], (float)a[i], sum[1], 2, 1, 0);
+  }
+}
 
 // Elements of a row that a wave takes at a time: two parts, 128 bytes.
 template <typename T>
@@ -74,18 +96,6 @@ __device__ __forceinline__ void wave_lds_fence() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// hidden of a slot: F values, for 16-bit types F high ones and F low ones.
-template <typename T>
-constexpr int kPieces = sizeof(T) == 4 ? 1 : 2;
-
-template <typename T>
-__device__ __forceinline__ void store_hidden(T* at, int64_t low, float v) {
-  const T high = (T)v;
-  *at = high;
-  if constexpr (kPieces<T> == 2)  // (an infinite one has no rest)
-    at[low] = __builtin_isinf((float)high) ? (T)0.f : (T)(v - (float)high);
-}
-
 // Workgroup (x, y): 16 hidden values of the slots of one expert, from 16 x on, y
 // itself, or by_slot the expert of slot y if it is the first of its slots.  HALF: 8
 // values from 8 x on, whose gates and values are the two halves of one tile, where
@@ -94,7 +104,7 @@ template <typename T, int NT, int STEPS, bool HALF>
 __global__ __launch_bounds__(kUpWaves * kWave, 4) void k_layer_up(
     const T* __restrict__ x, int64_t x_stride, const T* __restrict__ up,
     const int32_t* __restrict__ ids, int n, Divisor by_k, int C, int F, int E, bool by_slot,
-    T* __restrict__ hidden) {
+    float* __restrict__ hidden) {
   constexpr int kRows = HALF ? kTile / 2 : kTile;  // hidden values
   constexpr int kTiles = HALF ? 1 : 2;             // of rows: gates and values
   __shared__ int16_t s_slots[kMaxSlots];
@@ -181,7 +191,7 @@ __global__ __launch_bounds__(kUpWaves * kWave, 4) void k_layer_up(
         }
         const int f = f0 + i / 4 / kTile * 4 + i % 4, s = first + t * kTile + i / 4 % kTile;
         if (f < F && s < count)
-          store_hidden(hidden + (int64_t)s_slots[s] * kPieces<T> * F + f, F, a / (1.f + expf(-a)) * b);
+          hidden[(int64_t)s_slots[s] * F + f] = a / (1.f + expf(-a)) * b;
       }
     }
   }
@@ -196,7 +206,7 @@ __global__ __launch_bounds__(kUpWaves * kWave, 4) void k_layer_up(
 // write back the caches.)
 template <typename T, typename TW, int NT>
 __global__ __launch_bounds__(kDownWaves * kWave) void k_layer_down(
-    const T* __restrict__ hidden, const T* __restrict__ down, const TW* __restrict__ weights,
+    const float* __restrict__ hidden, const T* __restrict__ down, const TW* __restrict__ weights,
     const int32_t* __restrict__ ids, int n, int k, int C, int F, int E, int P,
     float* __restrict__ shares, T* __restrict__ out) {
   constexpr int kThreads = kDownWaves * kWave;
@@ -239,11 +249,13 @@ __global__ __launch_bounds__(kDownWaves * kWave) void k_layer_down(
   for (int item = blockIdx.y * kDownWaves + wave; item < groups * P; item += gridDim.y * kDownWaves) {
     const int group = item / P, part = item - group * P, end = s_first[group + 1];
     const T* row = down + ((int64_t)s_expert[group] * C + min(c0 + r, C - 1)) * F;
-    for (int first = s_first[group]; first < end; first += NT * kTile) {
-      int slots[NT];  // of this lane, -1 for none
+    // FEW: at most 4 FEW slots; otherwise up to 16 NT of them in a turn.
+    auto turn = [&](auto few, int first) {
+      constexpr int FEW = few.value, TILES = FEW > 0 ? 1 : NT;
+      int slots[TILES];  // of this lane, -1 for none
 #pragma unroll
-      for (int t = 0; t < NT; ++t) slots[t] = first + t * kTile + r < end ? s_slots[first + t * kTile + r] : -1;
-      Tile sum[NT] = {};
+      for (int t = 0; t < TILES; ++t) slots[t] = first + t * kTile + r < end ? s_slots[first + t * kTile + r] : -1;
+      Tile sum[FEW > 0 ? FEW : NT] = {};
       auto step = [&](auto check, auto steps, int k0) {
         constexpr bool CHECK = check.value;
         constexpr int S = 2 * steps.value;
@@ -252,18 +264,22 @@ __global__ __launch_bounds__(kDownWaves * kWave) void k_layer_down(
 #pragma unroll
         for (int i = 0; i < S; ++i) a[i] = part_at<T, CHECK>(row, place(i), F);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
+        for (int t = 0; t < TILES; ++t) {
           if (first + t * kTile >= end) break;
-          const T* high = hidden + (int64_t)slots[t] * kPieces<T> * F;
+          const float* slot = hidden + (int64_t)slots[t] * F;
 #pragma unroll
           for (int i = 0; i < S; ++i) {
-            Part<T> b[kPieces<T>] = {};
+            float b[N] = {};
             if (slots[t] >= 0) {
 #pragma unroll
-              for (int p = 0; p < kPieces<T>; ++p) b[p] = part_at<T, CHECK>(high + p * F, place(i), F);
-            }
+              for (int p = 0; p < N; p += 4) {
+                const Part<float> v = part_at<float, CHECK>(slot, place(i) + p, F);
 #pragma unroll
-            for (int p = 0; p < kPieces<T>; ++p) multiply(sum[t], a[i], b[p]);
+                for (int j = 0; j < 4; ++j) b[p + j] = v[j];
+              }
+            }
+            if constexpr (FEW > 0) multiply_few<T, FEW>(sum, a[i], b);
+            else multiply<T>(sum[t], a[i], b);
           }
         }
       };
@@ -271,18 +287,42 @@ __global__ __launch_bounds__(kDownWaves * kWave) void k_layer_down(
       constexpr std::integral_constant<int, 2> two;
       constexpr std::integral_constant<int, 1> single;
       int k0 = part * K;  // every P-th chunk
-      for (; k0 + 3 * P * K + K <= F; k0 += 4 * P * K) step(std::false_type{}, several, k0);
+      if constexpr (TILES == 1)
+        for (; k0 + 3 * P * K + K <= F; k0 += 4 * P * K) step(std::false_type{}, several, k0);
       for (; k0 + P * K + K <= F; k0 += 2 * P * K) step(std::false_type{}, two, k0);
       for (; k0 + K <= F; k0 += P * K) step(std::false_type{}, single, k0);
       if (k0 < F) step(std::true_type{}, single, k0);
+      if constexpr (FEW > 0) {
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        if (slots[t] < 0) continue;
-        const float w = (float)weights[slots[t]];
+        for (int u = 0; u < FEW; ++u) {
+          float v = 0.f;  // (lane 16 q + r keeps row r of slot q)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s_sums[(part * n + slots[t]) * kPitch + 4 * q + i] = w * sum[t][i];
+          for (int i = 0; i < 4; ++i) {
+            float all = sum[u][i];
+            all += __shfl_xor(all, 16, kWave);
+            all += __shfl_xor(all, 32, kWave);
+            v = q == i ? all : v;
+          }
+          if (first + 4 * u + q < end) {
+            const int slot = s_slots[first + 4 * u + q];
+            s_sums[(part * n + slot) * kPitch + r] = (float)weights[slot] * v;
+          }
+        }
+      } else {
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) {
+          if (slots[t] < 0) continue;
+          const float w = (float)weights[slots[t]];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s_sums[(part * n + slots[t]) * kPitch + 4 * q + i] = w * sum[t][i];
+        }
       }
-    }
+    };
+    const int begin = s_first[group];
+    if (end - begin <= 4) turn(std::integral_constant<int, 1>{}, begin);
+    else if (end - begin <= 8) turn(std::integral_constant<int, 2>{}, begin);
+    else
+      for (int first = begin; first < end; first += NT * kTile) turn(std::integral_constant<int, 0>{}, first);
   }
   __syncthreads();
   const int rows = n / k;
@@ -327,9 +367,7 @@ DownCut down_cut(int64_t n, int64_t C, int64_t F, int64_t E, int dtype) {
 }
 
 // Bytes of hidden, behind which the shares lie.
-size_t hidden_bytes(int64_t n, int64_t F) {
-  return (n * F * sizeof(float) + 15) / 16 * 16;  // (two 16-bit pieces take as much)
-}
+size_t hidden_bytes(int64_t n, int64_t F) { return (n * F * sizeof(float) + 15) / 16 * 16; }
 
 }  // namespace
 
@@ -349,11 +387,11 @@ hipError_t launch_expert_layer(int64_t rows, int32_t k, int64_t C, int64_t F, in
   const Divisor by_k = divisor(k);
   const DownCut cut = down_cut(n, C, F, n_experts, dtype);
   char* base = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(workspace) + 15) & ~uintptr_t(15));
+  float* hidden = reinterpret_cast<float*>(base);
   float* shares = reinterpret_cast<float*>(base + hidden_bytes(n, F));
   by_types(dtype, weight_dtype, [&](auto t, auto tw) {
     using T = decltype(t);
     using TW = decltype(tw);
-    T* hidden = reinterpret_cast<T*>(base);
     const bool by_slot = n <= n_experts;
     const int columns = by_slot ? n : n_experts;
     auto up_rows = [&](auto tiles, auto steps, auto half) {

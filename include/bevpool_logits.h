@@ -82,7 +82,9 @@ int bevpool_logprobs_backward(int64_t rows, int64_t V, int32_t k, int dtype, con
  * row's kept slots where renormalise != 0,
  *   loss[t] = sum_j q_j (log q_j - log p_id_j)
  * over the slots with q_j > 0 (0 where there are none); an id that occurs more
- * than once counts each time.  stats as above.
+ * than once counts each time.  Renormalised, what is added to all of a row's
+ * teacher has no part.  A NaN in a kept slot (renormalised, +inf too) makes the
+ * row's loss and gradient NaN.  stats as above.
  *
  * bevpool_distill_backward: grad[v] = grad_loss scale (Q p_v - sum_j [v = id_j] q_j),
  * Q = sum_j q_j, from the forward's stats; grad_logits as above.

@@ -91,7 +91,7 @@ struct DistillGradient {
       const int j = i * TEAM::kLanes + team.lane();
       if (j >= in.k) continue;
       ids[j] = slots.id[i];
-      values[j] = slot_gradient(slots, i, q, go, in.scale);
+      values[j] = slot_gradient(slots, i, go, in.scale);
     }
     return taught_gradient(m, S, q, go, in.scale);
   }
@@ -216,13 +216,13 @@ __global__ __launch_bounds__(kThreads) void k_short_step(LogitsRows in,
       const int j = i * L + lane;
       if (j >= marked) continue;
       ids[j] = slots.id[i];
-      values[j] = slot_gradient(slots, i, q, go, in.scale);
+      values[j] = slot_gradient(slots, i, go, in.scale);
     }
     const Soft a = soft_of<false>(team, held_row, held_row.largest(team.lane()), c);
     const Row p = row_of(a, in.scale);
     const RowGradient r = taught_gradient(p.m, p.S, q, go, in.scale);
     write_held<false>(team, held_row, row, out, r, in.V, c);
-    const float d = divergence(team, slots, p, q);
+    const float d = divergence(team, slots, p);
     if (lane == 0) {
       loss[t] = d;
       stats[2 * t] = p.m;
@@ -342,7 +342,7 @@ __global__ __launch_bounds__(L) void k_long_step(LogitsRows in, const float* __r
     const Taught q = taught(team, slots, in.renormalise);
     if (tid < k) {
       s_ids[tid] = id;
-      s_values[tid] = slot_gradient(slots, 0, q, go, in.scale);
+      s_values[tid] = slot_gradient(slots, 0, go, in.scale);
     }
     const Soft a = soft_of<false>(team, held_row, held_row.largest(team.lane()), c);
     const Row p = row_of(a, in.scale);
@@ -353,7 +353,7 @@ __global__ __launch_bounds__(L) void k_long_step(LogitsRows in, const float* __r
       s_gradients[tid] = base_of<false>(r, slots.x[0], c) + sum;
       s_next[tid] = atomicExch(&s_first[id < whole * N ? id / N % L : id - whole * N], tid);
     }
-    const float d = divergence(team, slots, p, q);
+    const float d = divergence(team, slots, p);
     if (tid == 0) {
       loss[t] = d;
       stats[2 * t] = p.m;

@@ -144,10 +144,10 @@ struct DistillRow {
     return own;
   }
   template <class TEAM>
-  __device__ __forceinline__ void finish(const TEAM& team, const LogitsRows& in, int64_t t, const Own& own,
+  __device__ __forceinline__ void finish(const TEAM& team, const LogitsRows& in, int64_t t, Own own,
                                          const Soft&, const Row& p) const {
-    const Taught q = taught(team, own, in.renormalise);
-    const float d = divergence(team, own, p, q);
+    taught(team, own, in.renormalise);
+    const float d = divergence(team, own, p);
     if (team.lane() != 0) return;
     stats[2 * t] = p.m;
     stats[2 * t + 1] = p.S;

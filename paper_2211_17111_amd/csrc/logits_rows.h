@@ -262,7 +262,7 @@ __device__ __forceinline__ int32_t id_at(const void* ids, int key_type, int64_t 
 template <int KS>
 struct Slots {
   int32_t id[KS];
-  float l[KS];  // log probability
+  float l[KS];  // log q: the teacher's log probability
   float x[KS];
 
   template <class TEAM>
@@ -286,15 +286,17 @@ struct Slots {
   }
 };
 
-// A teacher's side of a row: q_j = e^(l_j - shift), their sum and whether any
-// slot is kept.
+// A teacher's side of a row: the sum of q_j = e^(l_j) and whether any slot is kept.
 struct Taught {
-  float shift, mass;
+  float mass;
   bool any;
 };
 
+// (Renormalised, l_j becomes its difference from the row's largest, less the log of
+// the sum: two subtractions, since the sum of largest and log would be rounded by
+// 2^-24 of what is added to all l_j, which has no part.)
 template <class TEAM, int KS>
-__device__ __forceinline__ Taught taught(const TEAM& team, const Slots<KS>& slots, bool renormalise) {
+__device__ __forceinline__ Taught taught(const TEAM& team, Slots<KS>& slots, bool renormalise) {
   float top = -INFINITY, sum = 0.f, some = 0.f;
 #pragma unroll
   for (int i = 0; i < KS; ++i) {
@@ -302,41 +304,45 @@ __device__ __forceinline__ Taught taught(const TEAM& team, const Slots<KS>& slot
     some = slots.l[i] == -INFINITY ? some : 1.f;  // (a NaN is some)
   }
   some = team.max(some);
-  float shift = 0.f;
   if (renormalise) {
     top = team.max(top);
-    shift = top > -INFINITY ? top : 0.f;
+    top = top > -INFINITY ? top : 0.f;
+#pragma unroll
+    for (int i = 0; i < KS; ++i) slots.l[i] -= top;
   }
 #pragma unroll
-  for (int i = 0; i < KS; ++i) sum += expf(slots.l[i] - shift);
+  for (int i = 0; i < KS; ++i) sum += expf(slots.l[i]);
   sum = team.sum(sum);
-  if (!renormalise) return Taught{0.f, sum, some > 0.f};
-  return Taught{shift + logf(sum), 1.f, some > 0.f};
+  if (renormalise && some > 0.f) {
+    const float log_sum = logf(sum);
+#pragma unroll
+    for (int i = 0; i < KS; ++i) slots.l[i] -= log_sum;
+    sum = sum == sum ? 1.f : sum;
+  }
+  return Taught{sum, some > 0.f};
 }
 
 // Divergence of the row's distribution from the teacher's.  (The difference of
 // the log probabilities is taken in 64 bits: a student's that is beyond float32,
 // for a logit of the type's lowest number, may have a small share.)
 template <class TEAM, int KS>
-__device__ __forceinline__ float divergence(const TEAM& team, const Slots<KS>& slots, const Row& p,
-                                            const Taught& q) {
+__device__ __forceinline__ float divergence(const TEAM& team, const Slots<KS>& slots, const Row& p) {
   float loss = 0.f;
 #pragma unroll
   for (int i = 0; i < KS; ++i) {
     if (slots.l[i] == -INFINITY) continue;
-    const float own = expf(slots.l[i] - q.shift);
+    const float own = expf(slots.l[i]);
     const double behind = (double)p.scale * ((double)p.m - (double)slots.x[i]);
     if (own != 0.f)
-      loss += p.S == 0.f ? INFINITY : (float)(own * ((slots.l[i] - q.shift) + behind + p.log_S));
+      loss += p.S == 0.f ? INFINITY : (float)(own * (slots.l[i] + behind + p.log_S));
   }
   return team.sum(loss);
 }
 
 // What a slot adds to its token's gradient, go the row's outgoing one.
 template <int KS>
-__device__ __forceinline__ float slot_gradient(const Slots<KS>& slots, int i, const Taught& q,
-                                               float go, float scale) {
-  return slots.l[i] == -INFINITY ? 0.f : -go * scale * expf(slots.l[i] - q.shift);
+__device__ __forceinline__ float slot_gradient(const Slots<KS>& slots, int i, float go, float scale) {
+  return slots.l[i] == -INFINITY ? 0.f : -go * scale * expf(slots.l[i]);
 }
 
 }  // namespace bevpool

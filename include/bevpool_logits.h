@@ -8,7 +8,9 @@
  *              by itself or with the loss
  *
  * A row of logits x (V of them, of element type dtype) stands for the
- * distribution p = softmax(scale x), scale > 0 an inverse temperature.
+ * distribution p = softmax(scale x), scale > 0 an inverse temperature (scale log2 e
+ * has to be finite in float32: up to 2.35e38).  Values beyond float32 are infinite,
+ * the difference of two logits among them.
  *
  * Conventions are those of bevpool_rows.h (device pointers owned by the caller,
  * nothing allocated or synchronised, arguments validated before any HIP call,

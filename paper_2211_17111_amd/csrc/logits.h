@@ -3,6 +3,8 @@
 #pragma once
 
 #include <hip/hip_runtime.h>
+#include <float.h>
+#include <math.h>
 #include <stddef.h>
 #include <stdint.h>
 
@@ -12,6 +14,14 @@ namespace bevpool {
 
 constexpr int kMaxAlternatives = 64;  // of logprobs
 constexpr int kMaxTaught = 256;       // of distill
+
+// scale log2 e, as one float: its rounding is a relative 2^-25 of the scale.  A scale
+// for which it is infinite is refused: a row's largest logit would have exponent 0
+// times infinity.
+inline float exponent_factor(float scale) {
+  const double c = (double)scale * 1.4426950408889634;
+  return c > (double)FLT_MAX ? INFINITY : (float)c;
+}
 
 // Rows of logits and what goes with each row.
 struct LogitsRows {

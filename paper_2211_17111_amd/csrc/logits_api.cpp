@@ -47,6 +47,8 @@ int check_rows(int64_t stride, float scale, int key_type) {
   CHECK(check_stride(stride, "logits_stride"));
   if (!(scale > 0.f) || !std::isfinite(scale))
     return fail(BEVPOOL_EINVAL, "scale = %g must be positive and finite", scale);
+  if (!std::isfinite(bevpool::exponent_factor(scale)))
+    return fail(BEVPOOL_EINVAL, "scale = %g: scale log2 e exceeds float32", scale);
   return check_key_type(key_type);
 }
 

@@ -19,9 +19,6 @@ namespace bevpool {
 
 constexpr float kLn2 = 0.693147181f;
 
-// scale log2 e, as one float: its rounding is a relative 2^-25 of the scale.
-inline float exponent_factor(float scale) { return (float)((double)scale * 1.4426950408889634); }
-
 // A team of L threads (a power of two): within a wave up to 64, a workgroup
 // above.  `scratch`: LDS, a float for every wave of a workgroup's team.
 template <int L>

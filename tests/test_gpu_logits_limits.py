@@ -1,0 +1,35 @@
+"""Logits operators on the GPU at the ends of what they take."""
+
+import numpy as np
+import pytest
+import torch
+
+from _gpu import DEV
+from paper_2211_17111_amd import logits as lg
+from test_gpu_logits import INF, TYPES, _two_calls
+
+pytestmark = pytest.mark.gpu
+
+
+def test_the_largest_scales():
+    """All probability on the largest logits, shared by equal ones; nothing is NaN."""
+    for V in (50, 3001, 40000, 300007):
+        for dtype in TYPES:
+            for scale in (2.0 ** 127, 2.35e38):
+                x = torch.linspace(-4, 4, V, device=DEV).to(dtype).repeat(3, 1)
+                x[0, 3], x[1, 7], x[1, V - 1] = 9, 9, 9
+                x[2] = 1.5
+                r = lg.logprobs_forward(x, torch.tensor([3, 7, 0], device=DEV), 2, scale, True)
+                shares = torch.tensor([1.0, 2.0, V], dtype=torch.float64).log()
+                for got, want in ((r.logprob, -shares), (r.entropy, shares), (r.top[:, 0], -shares)):
+                    assert ((got.cpu().double() - want).abs() <= 2.0 ** -20 * (1 + want.abs())).all(), (V, dtype, scale)
+                assert r.top_ids.tolist() == [[3, int(x[0].float().cpu().sort(descending=True, stable=True).indices[1])],
+                                              [7, V - 1], [0, 1]]
+                assert (r.top[0, 1], r.lse[0]) == (-INF, INF)
+                ids = torch.tensor([[3, -1], [7, V - 1], [0, 1]], device=DEV)
+                teacher = torch.zeros((3, 2), device=DEV)
+                g = torch.full((3,), 0.5, device=DEV) / scale
+                for loss, grad in (_two_calls(g, x, ids, teacher, scale, True), lg.distill_step(g, x, ids, teacher, scale)):
+                    want = torch.tensor([0.0, 0.0, np.log(V / 2)], dtype=torch.float64)
+                    assert ((loss.cpu().double() - want).abs() <= 2.0 ** -20 * (1 + want)).all()
+                    assert torch.isfinite(grad).all() and (grad[:2].float().abs() < 1e-6).all()

@@ -209,3 +209,20 @@ def test_validation_under_sanitizers():
     out = res.stdout
     assert "AddressSanitizer" not in out and "runtime error" not in out, out[-4000:]
     assert res.returncode == 0 and " passed" in out, out[-4000:]
+
+
+def test_scales_whose_exponents_overflow_are_refused(lib):
+    """scale log2 e has to be finite in float32; the largest such scale and the smallest number are taken."""
+    def calls(scale):
+        rows = (0, 100, 3, 0)
+        at = (P, 100, scale, 0, P)
+        yield lib.bevpool_logprobs_forward(*rows, *at, P, P, P, P, P, P, None, 0, None)
+        yield lib.bevpool_logprobs_backward(*rows, *at, P, P, P, P, P, P, P, P, None)
+        yield lib.bevpool_distill_forward(*rows, *at, P, 1, P, P, None, 0, None)
+        yield lib.bevpool_distill_backward(*rows, P, *at, P, 1, P, P, None)
+        yield lib.bevpool_distill_step(*rows, P, *at, P, 1, P, P, P, None, 0, None)
+
+    for scale in (2.36e38, 3.4e38):
+        assert list(calls(scale)) == [EINVAL] * 5, scale
+    for scale in (2.35e38, 2.0 ** 127, 1e-45):
+        assert list(calls(scale)) == [OK] * 5, scale

@@ -41,9 +41,10 @@ extern "C" {
 
 /*
  * Log probabilities.  For every row t:
- *   stats[2 t], stats[2 t + 1]  the largest logit m (NaN not counted, -inf where
- *                 there is none) and S = sum_v e^(scale (x_v - m)) (0 for a row
- *                 without a distribution, NaN for one that holds a NaN or +inf);
+ *   stats[2 t], stats[2 t + 1]  the largest logit m (NaN not counted; -inf where
+ *                 there is none, and beside a NaN for float32's lowest number)
+ *                 and S = sum_v e^(scale (x_v - m)) (0 for a row without a
+ *                 distribution, NaN for one that holds a NaN or +inf);
  *   logprob[t]    scale (x_id - m) - log S for ids[t] (of key_type), 0 for an id
  *                 outside [0, V);
  *   lse[t]        scale m + log S;

@@ -242,8 +242,9 @@ struct Row {
 __device__ __forceinline__ Row row_of(float m, float S, float scale) {
   return Row{m, S, S == 0.f ? -INFINITY : logf(S), scale};
 }
+// (a row that only -inf and NaN are in leaves r where it began)
 __device__ __forceinline__ Row row_of(const Soft& a, float scale) {
-  return row_of(a.s == 0.f ? -INFINITY : a.r, a.s, scale);
+  return row_of(a.s > 0.f || a.r > kLowest ? a.r : -INFINITY, a.s, scale);
 }
 
 // Id i of an array of int32 or int64 ids, -1 when outside [0, V).

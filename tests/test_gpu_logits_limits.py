@@ -6,7 +6,7 @@ import torch
 
 from _gpu import DEV
 from paper_2211_17111_amd import logits as lg
-from test_gpu_logits import INF, TYPES, _two_calls
+from test_gpu_logits import INF, TYPES, Bounds, _logits, _np, _two_calls
 
 pytestmark = pytest.mark.gpu
 
@@ -33,3 +33,35 @@ def test_the_largest_scales():
                     want = torch.tensor([0.0, 0.0, np.log(V / 2)], dtype=torch.float64)
                     assert ((loss.cpu().double() - want).abs() <= 2.0 ** -20 * (1 + want)).all()
                     assert torch.isfinite(grad).all() and (grad[:2].float().abs() < 1e-6).all()
+
+
+def test_statistics():
+    """Every row's largest logit and sum, whatever else is asked for: also where the largest is the type's lowest, a
+    row holds a NaN or +inf, or nothing at all."""
+    nan = float("nan")
+    for V in (6, 118, 400, 3001, 9000, 40000, 300007):
+        for dtype in TYPES:
+            x = _logits(9, V, dtype, V, "masked" if V > 100 else "plain")
+            x[0] = -INF
+            x[1] = nan
+            x[2], x[2, V // 2] = -INF, nan
+            x[3, V - 1] = nan
+            x[4, V // 3] = INF
+            x[5], x[5, 1] = torch.finfo(dtype).min, -INF
+            x[6], x[6, V // 2] = -INF, -2.5
+            host = _np(x)
+            m = np.where(np.isnan(host), -INF, host).max(1)
+            whole = ~(np.isnan(host).any(1) | (host == INF).any(1))
+            b = Bounds(host[whole], 0.7)
+            with np.errstate(invalid="ignore"):
+                S = np.where(host[whole] > -INF, np.exp(0.7 * (host[whole] - m[whole, None])), 0).sum(1)
+            ids, teacher = torch.zeros((9, 2), dtype=torch.int32, device=DEV), torch.zeros((9, 2), device=DEV)
+            few = min(20, V // 2)
+            for stats in (lg.logprobs_forward(x, scale=0.7).stats, lg.logprobs_forward(x, None, 3, 0.7).stats,
+                          lg.logprobs_forward(x, None, 6, 0.7, True).stats, lg.logprobs_forward(x, scale=0.7, entropy=True).stats,
+                          lg.distill_forward(x, ids, teacher, 0.7)[1], lg.distill_forward(x, ids.repeat(1, few), teacher.repeat(1, few),
+                                                                                          0.7)[1]):
+                got = _np(stats)
+                assert np.array_equal(got[:, 0], m), (V, dtype, got[:, 0], m)
+                assert np.isnan(got[~whole, 1]).all()
+                assert (np.abs(got[whole, 1] - S) <= b.S * S).all(), (V, dtype)

@@ -14,10 +14,9 @@
  *
  * Conventions are those of bevpool_rows.h (device pointers owned by the caller,
  * nothing allocated or synchronised, arguments validated before any HIP call,
- * float32 sums rounded once, every output element written with one value in a
- * fixed order of operations, bitwise reproducible results, a matrix with a
- * stride has that many elements between its rows, pointers aligned to their
- * element, rows may be 0), and:
+ * float32 sums rounded once, a fixed order of operations, bitwise reproducible
+ * results, a matrix with a stride has that many elements between its rows,
+ * pointers aligned to their element, rows may be 0), and:
  *   - ids outside [0, V) are dropped, not errors: a position without a token, an
  *     alternative that the student does not know;
  *   - a logit of -inf has probability 0.  A row of nothing else has no
@@ -25,8 +24,11 @@
  *     alternatives -1, its gradient 0;
  *   - a NaN or +inf in a row makes that row's values NaN, but for those of
  *     dropped ids;
- *   - a row whose outgoing gradients are zero or belong to dropped ids has a
- *     gradient of zeros whatever it holds (padding is not read);
+ *   - a row whose outgoing gradients are zero or belong to dropped ids (padding)
+ *     has a gradient of zeros whatever it holds;
+ *   - in gradients, an element of a token with an outgoing gradient of its own, or
+ *     of one that is taught, may be stored twice: with its vector and, after that,
+ *     with its value;
  *   - limits: rows < 2^31, V <= 2^20, k <= V, and k <= 64 in logprobs, <= 256 in
  *     distill.
  */

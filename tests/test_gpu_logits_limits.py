@@ -4,9 +4,9 @@ import numpy as np
 import pytest
 import torch
 
-from _gpu import DEV
+from _gpu import DEV, say
 from paper_2211_17111_amd import logits as lg
-from test_gpu_logits import INF, TYPES, Bounds, _logits, _np, _two_calls
+from test_gpu_logits import CHAIN, F32, INF, TYPES, U, Bounds, _logits, _np, _two_calls
 
 pytestmark = pytest.mark.gpu
 
@@ -65,3 +65,47 @@ def test_statistics():
                 assert np.array_equal(got[:, 0], m), (V, dtype, got[:, 0], m)
                 assert np.isnan(got[~whole, 1]).all()
                 assert (np.abs(got[whole, 1] - S) <= b.S * S).all(), (V, dtype)
+
+
+def _mixed(T, V, dtype, seed):
+    """Rows of five kinds in turn: normal; 9 values only; equal; the best at a row's end; and at its beginning."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    x = torch.randn((T, V), generator=g, device=DEV) * 3
+    x[1::5] = torch.randint(-4, 5, (len(range(1, T, 5)), V), generator=g, device=DEV).float() * 0.5
+    x[2::5] = 1.5
+    x[3::5] = torch.linspace(-9, 9, V, device=DEV)
+    x[4::5] = torch.linspace(9, -9, V, device=DEV)
+    x[7::10, : V // 2] = -INF
+    return x.to(dtype)
+
+
+@pytest.mark.parametrize("k", [1, 20, 64])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,batches,more", [(1030, 16, 0), (1030, 16, -1), (1030, 16, 1), (1030, 16, 8), (1030, 16, 4001), (1100, 5, 0),
+                                            (1030, 8, 77), (1500, 11, 3), (400, 16, 0), (300, 40, 5), (1025, 33, 0)])
+def test_alternatives_of_long_parts(T, batches, more, dtype, k):
+    """Parts of 5 to 16 batches of 1024 vectors, the most that a part with alternatives has, and rows just longer, which
+    are cut though there are many of them; all rows' choices, candidates beyond the list among them."""
+    V = batches * 1024 * (4 if dtype == F32 else 8) + more
+    if batches > 16:
+        T //= 4 if dtype != F32 else 2
+    say(f"alternatives T={T} V={V} k={k} {dtype}")
+    x = _mixed(T, V, dtype, V + k)
+    r = lg.logprobs_forward(x, None, k, 0.9, entropy=k == 20)
+    place = torch.arange(V - 1, -1, -1, device=DEV)
+    for a in range(0, T, 128):
+        l = x[a:a + 128].float() + 0.0  # (-0 + 0 = 0)
+        bits = l.view(torch.int32)
+        order = (bits ^ ((bits >> 31) & 0x7FFFFFFF)).long() * (1 << 20) + place  # larger logits, lower places first
+        at = torch.topk(order, k, 1).indices
+        d = l.double()
+        m = d.max(1, keepdim=True).values
+        e = torch.exp(0.9 * (d - m))
+        S = e.sum(1, keepdim=True)
+        mean = torch.where(e > 0, e * 0.9 * (m - d), 0.0).sum(1, keepdim=True) / S
+        own = 0.9 * (m - d.gather(1, at))
+        assert torch.equal(r.top_ids[a:a + 128].long(), at), a
+        bound = U * (3.5 * own + 3 * S.log() + 2.5 * mean + 4 * CHAIN(V) + 8)
+        assert ((r.top[a:a + 128].double() - (-own - S.log())).abs() <= bound).all(), a
+        lse = (0.9 * m + S.log())[:, 0]
+        assert ((r.lse[a:a + 128].double() - lse).abs() <= U * (4 * lse.abs() + 8 * S[:, 0].log()) + bound[:, 0]).all(), a

@@ -5,7 +5,7 @@
 //
 // A logit is read and its gradient written once, and that is what bounds them:
 // 8192 rows of 65,536 bfloat16 take 412 us, 5.2 TB/s (a copy reaches 5.06); loss and
-// gradient in one call read and write as much in 489.  The marked tokens are written
+// gradient in one call read and write as much in 466.  The marked tokens are written
 // again after their vectors.
 
 #include "logits.h"

@@ -450,9 +450,12 @@ constexpr int kShort = 512;
 
 // How rows of `vectors` are cut: into parts of whole batches, so that there are
 // about four workgroups to a compute unit, and batches enough for the maxima of a
-// part that alternatives are chosen from.  A part has at least kLeastBatches: of
-// two launches the second costs more than these take (one row of 32,000 bfloat16
-// with 8 alternatives 12.2 us whole, 15.7 in four parts).
+// part that alternatives are chosen from.  A part has at least kLeastBatches: a row
+// of no more is not cut, since a second launch costs more than these take (one row
+// of 32,000 bfloat16 with 8 alternatives 8.9 us whole, 11.9 in two parts, 11.2 in
+// four).  For rows that are cut anyway the least length matters less; microseconds
+// with at least 2, 4 and 8 batches: one row of 131,072 with 8 alternatives 11.8,
+// 12.7 and 14.1, 16 with 20 14.0, 15.6 and 17.9, 128 19.7, 18.8 and 20.1.
 constexpr int kLeastBatches = 4;
 struct Cut {
   int32_t count, length;

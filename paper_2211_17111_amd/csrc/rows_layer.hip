@@ -8,8 +8,8 @@
 // are read once for all slots of an expert, and what bounds the layer is reading
 // them.  A wave takes 128 bytes of each of its 16 rows at a time; the waves of a
 // workgroup take turns along the rows, and their sums are joined in LDS.  64 tokens,
-// 8 of 128 experts, C 4096, F 1280, bfloat16: up 2.6 GB in 475 us (5.5 TB/s), down 1.3
-// GB in 320 (4.2).
+// 8 of 128 experts, C 4096, F 1280, bfloat16: up 2.6 GB in 474 us (5.5 TB/s), down 1.3
+// GB in 317 (4.2).
 //
 // hidden lies between the launches, in float32 whatever the layer's type, and meets
 // down's rows in float32 products: a sum's intermediate has float32's range and digits,
@@ -202,7 +202,8 @@ __global__ __launch_bounds__(kUpWaves * kWave, 4) void k_layer_up(
 // expert with slots (a group), and one of P parts of its rows' chunks.  Where
 // several workgroups share the items (few columns would leave compute units idle),
 // their sums go to `shares`, which a third launch adds up in their order.  (Adding
-// up by the last of them to arrive took 97 us instead of 17 at one token: its fences
+// up by the last of them to arrive took 97 us where this launch took 17, at one token
+// of 6 experts, C 2048, F 1024, where it takes 11 now and the third 3: its fences
 // write back the caches.)
 template <typename T, typename TW, int NT>
 __global__ __launch_bounds__(kDownWaves * kWave) void k_layer_down(

@@ -17,7 +17,8 @@ forms.  A layer of experts reads
     y = experts(rows, plan.offsets)               #   offsets[e] .. offsets[e+1]
     out = combine(y, weights, plan)
 
-and of a few tokens, without gradients, in one call (gated experts, two launches):
+and of a few tokens, without gradients, in one call (gated experts; two launches, three where
+columns are few):
 
     out = expert_layer_forward(x, up, down, *route_forward(logits, k))
 
